@@ -342,6 +342,38 @@ int dmoe_ln_act_bwd(const dmoe_dims* dims, const int32_t* offsets, const void* h
                     const void* gamma, const void* beta, const void* da, void* dh, void* dgamma,
                     void* dbeta, void* stream);
 
+/* ------------------------------------------------------------------------------
+ * Around the layer.  A DMoE layer that replaces a Transformer's feed-forward block sits in
+ * the sub-layer  s = x + r,  n = LN(s),  out = s + DMoE(n).
+ * ------------------------------------------------------------------------------ */
+
+/* Layer normalisation of T rows of D features (dims->T, D and dtype; the other fields only
+ * have to be valid), D at most 16384, with the residual added first:
+ *   s = x + res (rounded to the layer dtype, as it is stored; s = x where res is NULL),
+ *   mean = mean_f(s),  rstd = 1 / sqrt(mean_f((s - mean)^2) + 1e-5),
+ *   y = gamma (s - mean) rstd + beta.
+ *   x [T, D], res [T, D] or NULL, gamma [D], beta [D] or NULL (no shift)
+ * outputs
+ *   s_out [T, D]  s; NULL exactly where res is NULL.  May be x or res
+ *   y     [T, D]  may be x or res, not s_out
+ *   stats [T, 2]  fp32 (mean, rstd) of each row, or NULL
+ * Uses workspace: no. */
+int dmoe_layer_norm_fwd(const dmoe_dims* dims, const void* x, const void* res, const void* gamma,
+                        const void* beta, void* s_out, void* y, float* stats, void* stream);
+
+/* Backward of dmoe_layer_norm_fwd from the gradient dy of y, and dres, the gradient that
+ * reaches s past the normalisation (the residual's), or NULL for none:
+ *   n = (s - mean) rstd,  dn = dy gamma,
+ *   dx = rstd (dn - mean_f(dn) - n mean_f(dn n)) + dres   (the gradient of x and of res),
+ *   dgamma = sum_t dy n,  dbeta = sum_t dy.
+ *   s [T, D] (s_out, or x where there was no residual), stats [T, 2], gamma [D], dy, dres [T, D]
+ * outputs: dx [T, D] (may be dy, dres or s), dgamma [D], dbeta [D] or NULL; T = 0 gives zero
+ * dgamma and dbeta.  ws: dmoe_layer_norm_workspace_bytes(dims) bytes (0 for invalid dims). */
+int dmoe_layer_norm_bwd(const dmoe_dims* dims, const void* s, const float* stats, const void* gamma,
+                        const void* dy, const void* dres, void* dx, void* dgamma, void* dbeta, void* ws,
+                        void* stream);
+size_t dmoe_layer_norm_workspace_bytes(const dmoe_dims* dims);
+
 #ifdef __cplusplus
 }
 #endif

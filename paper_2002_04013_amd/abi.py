@@ -25,6 +25,7 @@ EXPORTS = (
     "dmoe_expert_ffn_bwd", "dmoe_dispatch_bwd", "dmoe_expert_ffn_bwd_recompute", "dmoe_expert_ffn_bwd_sgd",
     "dmoe_expert_ffblock_fwd", "dmoe_expert_ffblock_bwd", "dmoe_ln_act_fwd", "dmoe_ln_act_bwd",
     "dmoe_trace_begin", "dmoe_trace_end", "dmoe_expert_ffn_fwd_noalloc", "dmoe_ffn_workspace_bytes",
+    "dmoe_layer_norm_fwd", "dmoe_layer_norm_bwd", "dmoe_layer_norm_workspace_bytes",
 )
 
 # parameters of the feed-forward block expert, in dmoe_ffblock_params order
@@ -94,6 +95,9 @@ def load(path=LIB_PATH):
                                             ctypes.c_int]),
         "dmoe_trace_end": (ctypes.c_int, []),
         "dmoe_expert_ffn_fwd_noalloc": (ctypes.c_int, [pd] + [_P] * 10),
+        "dmoe_layer_norm_fwd": (ctypes.c_int, [pd] + [_P] * 8),
+        "dmoe_layer_norm_bwd": (ctypes.c_int, [pd] + [_P] * 10),
+        "dmoe_layer_norm_workspace_bytes": (ctypes.c_size_t, [pd]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -250,6 +254,21 @@ def dmoe_ln_act_bwd(dims, offsets, h, stats, gamma, beta, da, dh, dgamma, dbeta,
     _check(load().dmoe_ln_act_bwd(ctypes.byref(dims), _ptr(offsets), _ptr(h), _ptr(stats), _ptr(gamma),
                                   _ptr(beta), _ptr(da), _ptr(dh), _ptr(dgamma), _ptr(dbeta), _stream(stream)),
            "dmoe_ln_act_bwd")
+
+
+def layer_norm_workspace_bytes(dims):
+    return int(load().dmoe_layer_norm_workspace_bytes(ctypes.byref(dims)))
+
+
+def dmoe_layer_norm_fwd(dims, x, res, gamma, beta, s_out, y, stats=None, stream=None):
+    _check(load().dmoe_layer_norm_fwd(ctypes.byref(dims), _ptr(x), _ptr(res), _ptr(gamma), _ptr(beta), _ptr(s_out),
+                                      _ptr(y), _ptr(stats), _stream(stream)), "dmoe_layer_norm_fwd")
+
+
+def dmoe_layer_norm_bwd(dims, s, stats, gamma, dy, dres, dx, dgamma, dbeta, ws, stream=None):
+    _check(load().dmoe_layer_norm_bwd(ctypes.byref(dims), _ptr(s), _ptr(stats), _ptr(gamma), _ptr(dy), _ptr(dres),
+                                      _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), _stream(stream)),
+           "dmoe_layer_norm_bwd")
 
 
 class Trace:

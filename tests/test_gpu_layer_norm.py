@@ -1,0 +1,265 @@
+"""Layer normalisation of the sub-layer, forward and backward, against the formulas in 64
+bits (and the backward against differences of the 64-bit forward), with elementwise error
+bounds: u = 2^-24 per fp32 operation, a row sum of at most 32 adds in a lane, 6 exchanges
+and 16 waves, one rounding of the result to the layer's type (half a step)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2002_04013_amd import abi
+
+U = 2.0 ** -24
+ROW = 64.0                       # fp32 operations on the way of one row sum, rounded up
+EPS = 1e-5
+
+
+def _half_step(dtype):
+    return 0.0 if dtype == "f32" else torch.finfo(torch.bfloat16).eps / 2
+
+
+def _store(a, dtype):
+    return a.to(torch.float32 if dtype == "f32" else torch.bfloat16)
+
+
+def _fwd64(s, gamma, beta):
+    mean = s.mean(1, keepdim=True)
+    rstd = 1.0 / torch.sqrt(((s - mean) ** 2).mean(1, keepdim=True) + EPS)
+    return gamma * (s - mean) * rstd + beta, mean, rstd
+
+
+def _inputs(T, D, dtype, seed, offset=0.0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: _store(torch.randn(*s, generator=g), dtype)
+    q = dict(x=_store(torch.randn(T, D, generator=g) + offset, dtype), res=r(T, D), gamma=r(D), beta=r(D), dy=r(T, D),
+             dres=r(T, D))
+    return q
+
+
+def _assert_within(got, want, bound, name):
+    got = got.double().cpu()
+    assert got.shape == want.shape
+    err = (got - want).abs()
+    worst = (err / bound.clamp(min=1e-300)).max().item() if err.numel() else 0.0
+    assert (err <= bound).all(), f"{name}: {worst:.3g} of the bound"
+
+
+def _dims(T, D, dtype):
+    return abi.make_dims(T, D, 64, 1, 1, 1, dtype, "relu")
+
+
+# every lane group (8 .. 64 lanes, a wave of 2 and 4 chunks, 4, 8 and 16 waves) and rows of one to
+# several rounds of the grid; widths that leave lanes without a chunk
+SIZES = [(1, 64), (3, 64), (257, 192), (70, 320), (33, 448), (1, 960), (515, 960), (7, 1024), (9000, 64), (6, 1984),
+         (5, 2048), (2100, 2112), (3, 4096), (4, 6592), (2, 8192), (3, 8256), (5, 16384)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("res", [False, True])
+@pytest.mark.parametrize("T,D", SIZES)
+def test_forward(T, D, dtype, res):
+    q = _inputs(T, D, dtype, 1000 * T + D, offset=3.0)
+    t = {n: v.cuda() for n, v in q.items()}
+    y = torch.full_like(t["x"], float("nan"))
+    s = torch.full_like(y, float("nan")) if res else None
+    stats = torch.full((T, 2), float("nan"), device="cuda")
+    abi.dmoe_layer_norm_fwd(_dims(T, D, dtype), t["x"], t["res"] if res else None, t["gamma"], t["beta"], s, y, stats)
+    s64 = q["x"].double()
+    if res:
+        want = (q["x"].float() + q["res"].float()).to(q["x"].dtype)
+        assert torch.equal(s.cpu(), want)              # one fp32 addition, one rounding
+        s64 = want.double()
+    gamma, beta = q["gamma"].double(), q["beta"].double()
+    y64, mean, rstd = _fwd64(s64, gamma, beta)
+    mean_err = ROW * U * s64.abs().mean(1, keepdim=True)
+    _assert_within(stats[:, :1], mean, mean_err, "mean")
+    # the variance: a sum about a mean that is off by mean_err, relative error ROW u plus the square of that
+    rel = (ROW + 8) * U + (mean_err * rstd) ** 2
+    _assert_within(stats[:, 1:], rstd, rstd * rel, "rstd")
+    n = (s64 - mean) * rstd
+    err = gamma.abs() * (n.abs() * (rel + 4 * U) + mean_err * rstd) + 2 * U * (gamma * n).abs() + U * beta.abs()
+    _assert_within(y, y64, err + _half_step(dtype) * (y64.abs() + err) + U * y64.abs(), "y")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("res", [False, True])
+@pytest.mark.parametrize("T,D", SIZES)
+def test_backward(T, D, dtype, res):
+    q = _inputs(T, D, dtype, 77 * T + D)
+    t = {n: v.cuda() for n, v in q.items()}
+    dims = _dims(T, D, dtype)
+    s64, gamma, dy = q["x"].double(), q["gamma"].double(), q["dy"].double()
+    _, mean, rstd = _fwd64(s64, gamma, torch.zeros(D, dtype=torch.float64))
+    stats = torch.cat((mean, rstd), 1).float()
+    ws = torch.full((abi.layer_norm_workspace_bytes(dims),), 255, dtype=torch.uint8, device="cuda")
+    dx = torch.full_like(t["x"], float("nan"))
+    dg, db = torch.full_like(t["gamma"], float("nan")), torch.full_like(t["gamma"], float("nan"))
+    abi.dmoe_layer_norm_bwd(dims, t["x"], stats.cuda(), t["gamma"], t["dy"], t["dres"] if res else None, dx, dg, db, ws)
+    # from the fp32 statistics, as the call has them
+    mean, rstd = stats[:, :1].double(), stats[:, 1:].double()
+    n = (s64 - mean) * rstd
+    n_err = 2 * U * (s64.abs() + mean.abs()) * rstd
+    dn = dy * gamma
+    m1, m2 = dn.mean(1, keepdim=True), (dn * n).mean(1, keepdim=True)
+    m1_err = ROW * U * dn.abs().mean(1, keepdim=True)
+    m2_err = (dn.abs() * n_err).mean(1, keepdim=True) + (ROW + 2) * U * (dn * n).abs().mean(1, keepdim=True)
+    want = rstd * (dn - m1 - n * m2)
+    err = rstd * (m1_err + n.abs() * m2_err + n_err * m2.abs() + 6 * U * (dn.abs() + m1.abs() + (n * m2).abs()))
+    if res:
+        want = want + q["dres"].double()
+        err = err + U * want.abs()
+    _assert_within(dx, want, err + _half_step(dtype) * (want.abs() + err) + U * want.abs(), "dx")
+    # a column's sum: its rows in a lane (at most T / 512 of them one after another), the block's groups (at most
+    # 32), the blocks' slices (at most 32 blocks each, 32 slices)
+    depth = T / 512 + 1 + 32 + 32 + 32 + 4
+    for got, ref, ab, name in ((dg, (dy * n).sum(0), (dy * n).abs().sum(0) * depth * U + (dy.abs() * n_err).sum(0), "dgamma"),
+                               (db, dy.sum(0), dy.abs().sum(0) * depth * U, "dbeta")):
+        _assert_within(got, ref, ab + _half_step(dtype) * (ref.abs() + ab) + U * ref.abs(), name)
+
+
+def test_backward_formula_against_differences():
+    """The formulas the GPU results are held to, against central differences of the 64-bit forward."""
+    g = torch.Generator().manual_seed(4)
+    T, D = 3, 64
+    s, gamma, beta, dy = (torch.randn(*sh, generator=g, dtype=torch.float64) for sh in ((T, D), (D,), (D,), (T, D)))
+    _, mean, rstd = _fwd64(s, gamma, beta)
+    n, dn = (s - mean) * rstd, dy * gamma
+    dx = rstd * (dn - dn.mean(1, keepdim=True) - n * (dn * n).mean(1, keepdim=True))
+    f = lambda a, b, c: (_fwd64(a, b, c)[0] * dy).sum().item()
+    h = 1e-6
+    for i, j in ((0, 0), (1, 17), (2, 63)):
+        e = torch.zeros_like(s); e[i, j] = h
+        # truncation h^2 f''' / 6 and rounding 2^-52 |f| / h, both below 1e-7 here
+        assert abs((f(s + e, gamma, beta) - f(s - e, gamma, beta)) / (2 * h) - dx[i, j].item()) < 1e-7
+        e = torch.zeros_like(gamma); e[j] = h
+        assert abs((f(s, gamma + e, beta) - f(s, gamma - e, beta)) / (2 * h) - (dy * n).sum(0)[j].item()) < 1e-7
+        assert abs((f(s, gamma, beta + e) - f(s, gamma, beta - e)) / (2 * h) - dy.sum(0)[j].item()) < 1e-7
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_over_inputs(dtype):
+    """s over x or res, y over x or res, dx over dy, dres or s: the results of separate buffers, bit for bit."""
+    T, D = 300, 960
+    t = {n: v.cuda() for n, v in _inputs(T, D, dtype, 5).items()}
+    dims = _dims(T, D, dtype)
+    s, y, st = torch.empty_like(t["x"]), torch.empty_like(t["x"]), torch.empty(T, 2, device="cuda")
+    abi.dmoe_layer_norm_fwd(dims, t["x"], t["res"], t["gamma"], t["beta"], s, y, st)
+    for over_s, over_y in (("x", "res"), ("res", "x")):
+        c = {n: t[n].clone() for n in ("x", "res")}
+        abi.dmoe_layer_norm_fwd(dims, c["x"], c["res"], t["gamma"], t["beta"], c[over_s], c[over_y], None)
+        assert torch.equal(c[over_s], s) and torch.equal(c[over_y], y)
+    ws = torch.empty(abi.layer_norm_workspace_bytes(dims), dtype=torch.uint8, device="cuda")
+    dx, dg, db = torch.empty_like(s), torch.empty_like(t["gamma"]), torch.empty_like(t["gamma"])
+    abi.dmoe_layer_norm_bwd(dims, s, st, t["gamma"], t["dy"], t["dres"], dx, dg, db, ws)
+    for over in ("dy", "dres", "s"):
+        c = dict(dy=t["dy"].clone(), dres=t["dres"].clone(), s=s.clone())
+        dg2 = torch.empty_like(dg)
+        abi.dmoe_layer_norm_bwd(dims, c["s"], st, t["gamma"], c["dy"], c["dres"], c[over], dg2, None, ws)
+        assert torch.equal(c[over], dx) and torch.equal(dg2, dg)
+
+
+@pytest.mark.gpu
+def test_no_rows_no_shift_and_not_finite_rows():
+    dims = _dims(0, 128, "f32")
+    e = lambda *s: torch.full(s, 7.0, device="cuda")
+    dg, db = e(128), e(128)
+    ws = torch.empty(abi.layer_norm_workspace_bytes(dims), dtype=torch.uint8, device="cuda")
+    raw, p = abi.load(), abi._ptr
+    assert raw.dmoe_layer_norm_bwd(abi.ctypes.byref(dims), None, None, None, None, None, None, p(dg), p(db), p(ws),
+                                   abi._stream()) == 0
+    assert not dg.any() and not db.any()
+    # a constant row (zero variance) gives beta; beta NULL gives no shift
+    dims = _dims(4, 128, "f32")
+    x = torch.randn(4, 128, device="cuda")
+    x[1] = 5.0
+    x[2, 7] = float("inf")
+    x[3, 9] = float("nan")
+    gamma, beta, y = e(128), torch.randn(128, device="cuda"), e(4, 128)
+    abi.dmoe_layer_norm_fwd(dims, x, None, gamma, beta, None, y)
+    assert torch.equal(y[1], beta)
+    assert torch.isfinite(y[:2]).all() and torch.isnan(y[2]).all() and torch.isnan(y[3]).all()
+    y2 = e(4, 128)
+    abi.dmoe_layer_norm_fwd(dims, x, None, gamma, None, None, y2)
+    assert not y2[1].any()
+    assert (y2[0] + beta - y[0]).abs().max() <= 4 * U * 7 * 12 + U * 12
+
+
+@pytest.mark.gpu
+def test_stream_argument_and_graph_replay():
+    """Forward and backward on another stream than the current one, and captured and replayed with other work in
+    between: the eager results, bit for bit."""
+    T, D = 777, 1024
+    t = {n: v.cuda() for n, v in _inputs(T, D, "bf16", 9).items()}
+    dims = _dims(T, D, "bf16")
+    o = {n: torch.empty_like(t["x"]) for n in ("s", "y", "dx")}
+    o.update(st=torch.empty(T, 2, device="cuda"), dg=torch.empty_like(t["gamma"]), db=torch.empty_like(t["gamma"]))
+    ws = torch.empty(abi.layer_norm_workspace_bytes(dims), dtype=torch.uint8, device="cuda")
+
+    def step(stream=None):
+        abi.dmoe_layer_norm_fwd(dims, t["x"], t["res"], t["gamma"], t["beta"], o["s"], o["y"], o["st"], stream=stream)
+        abi.dmoe_layer_norm_bwd(dims, o["s"], o["st"], t["gamma"], t["dy"], t["dres"], o["dx"], o["dg"], o["db"], ws,
+                                stream=stream)
+
+    step()
+    torch.cuda.synchronize()
+    ref = {n: v.clone() for n, v in o.items()}
+    side = torch.cuda.Stream()
+    for v in o.values():
+        v.fill_(3)
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    assert all(torch.equal(o[n], ref[n]) for n in o)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for v in o.values():
+            v.fill_(3)
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o[n], ref[n]) for n in o)
+
+
+@pytest.mark.parametrize("what,rc", [
+    ("ok", 0), ("no x", -1), ("no gamma", -1), ("no y", -1), ("res without s", -1), ("s without res", -1),
+    ("y over s", -1), ("x off by 8 bytes", -2), ("stats off by 8 bytes", -2), ("D above 16384", -2), ("T < 0", -1)])
+def test_forward_refusals_on_host(what, rc):
+    """Refused before any device work; the addresses are never read.  ("ok" with T = 0 launches nothing.)"""
+    P = lambda n, off=0: abi.ctypes.c_void_p((n << 20) + off)
+    a = dict(x=P(1), res=P(2), gamma=P(3), beta=P(4), s=P(5), y=P(6), stats=P(7))
+    T, D = (0 if what == "ok" else -1 if what == "T < 0" else 8), (16448 if what == "D above 16384" else 64)
+    a.update({"no x": dict(x=None), "no gamma": dict(gamma=None), "no y": dict(y=None), "res without s": dict(s=None),
+              "s without res": dict(res=None), "y over s": dict(y=P(5)), "x off by 8 bytes": dict(x=P(1, 8)),
+              "stats off by 8 bytes": dict(stats=P(7, 8))}.get(what, {}))
+    dims = _dims(T, D, "bf16")
+    got = abi.load().dmoe_layer_norm_fwd(abi.ctypes.byref(dims), *a.values(), None)
+    assert got == rc
+    if what in ("D above 16384", "T < 0"):
+        assert abi.layer_norm_workspace_bytes(dims) == 0
+
+
+@pytest.mark.parametrize("what,rc", [
+    ("no s", -1), ("no stats", -1), ("no gamma", -1), ("no dy", -1), ("no dx", -1), ("no dgamma", -1), ("no ws", -1),
+    ("dres off by 2 bytes", -2), ("D above 16384", -2)])
+def test_backward_refusals_on_host(what, rc):
+    P = lambda n, off=0: abi.ctypes.c_void_p((n << 20) + off)
+    a = {n: P(i + 1) for i, n in enumerate(("s", "stats", "gamma", "dy", "dres", "dx", "dgamma", "dbeta", "ws"))}
+    if what.startswith("no "):
+        a[what[3:]] = None
+    if what == "dres off by 2 bytes":
+        a["dres"] = P(5, 2)
+    dims = _dims(8, 16448 if what == "D above 16384" else 64, "f32")
+    assert abi.load().dmoe_layer_norm_bwd(abi.ctypes.byref(dims), *a.values(), None) == rc
+
+
+def test_workspace_covers_the_blocks():
+    """Two fp32 rows of D sums for each block; at most 1024 blocks, and one for few rows."""
+    for T, D, dtype in ((1, 64, "bf16"), (100000, 4096, "bf16"), (77, 960, "f32"), (5000, 16384, "f32"), (0, 64, "f32")):
+        n = abi.layer_norm_workspace_bytes(_dims(T, D, dtype))
+        assert n % (8 * D) == 0 and 8 * D <= n <= max(1, min(T, 1024)) * 8 * D
+    assert np.all([abi.layer_norm_workspace_bytes(_dims(4, d, "bf16")) == 0 for d in (16448, 65, 0)])
