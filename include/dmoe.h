@@ -374,6 +374,26 @@ int dmoe_layer_norm_bwd(const dmoe_dims* dims, const void* s, const float* stats
                         void* stream);
 size_t dmoe_layer_norm_workspace_bytes(const dmoe_dims* dims);
 
+/* The whole layer for a few tokens (serving), T at most 64:
+ *   y = res + DMoE(x)   (y = DMoE(x) where res is NULL),
+ * with the choice of experts, weights and expert blocks of dmoe_gate_topk and
+ * dmoe_expert_ffn_fwd: the same idx, w and y as gate, dispatch, experts and combine give, up
+ * to rounding (the gate's scores are exact for every token; h and the experts' outputs are kept
+ * in fp32, the activations in the layer dtype).  Reads the weights of the chosen alive experts
+ * once and keeps nothing for a backward pass.
+ *   x [T, D], Wg [d*M, D], bg [d*M] or NULL, alive [N] or NULL,
+ *   W1 [N, H, D], b1 [N, H], W2 [N, D, H], b2 [N, D], res [T, D] or NULL
+ * outputs
+ *   idx [T, k], w [T, k]  as dmoe_gate_topk's
+ *   y   [T, D]            may be x or res; res (or 0) for a token with no alive expert
+ * More than 64 tokens: DMOE_EUNSUPPORTED.  dims->flags as for dmoe_gate_topk.  ws:
+ * dmoe_layer_few_workspace_bytes(dims) bytes (0 for invalid dims and more than 64 tokens). */
+int dmoe_layer_few_fwd(const dmoe_dims* dims, const void* x, const void* Wg, const void* bg,
+                       const uint8_t* alive, const void* W1, const void* b1, const void* W2,
+                       const void* b2, const void* res, int32_t* idx, float* w, void* y, void* ws,
+                       void* stream);
+size_t dmoe_layer_few_workspace_bytes(const dmoe_dims* dims);
+
 #ifdef __cplusplus
 }
 #endif

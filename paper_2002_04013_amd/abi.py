@@ -26,7 +26,10 @@ EXPORTS = (
     "dmoe_expert_ffblock_fwd", "dmoe_expert_ffblock_bwd", "dmoe_ln_act_fwd", "dmoe_ln_act_bwd",
     "dmoe_trace_begin", "dmoe_trace_end", "dmoe_expert_ffn_fwd_noalloc", "dmoe_ffn_workspace_bytes",
     "dmoe_layer_norm_fwd", "dmoe_layer_norm_bwd", "dmoe_layer_norm_workspace_bytes",
+    "dmoe_layer_few_fwd", "dmoe_layer_few_workspace_bytes",
 )
+
+FEW_TOKENS = 64      # most tokens of dmoe_layer_few_fwd
 
 # parameters of the feed-forward block expert, in dmoe_ffblock_params order
 FFBLOCK_PARAMS = ("W1", "b1", "g1", "be1", "W2", "b2", "g2", "be2", "W3", "b3")
@@ -98,6 +101,8 @@ def load(path=LIB_PATH):
         "dmoe_layer_norm_fwd": (ctypes.c_int, [pd] + [_P] * 8),
         "dmoe_layer_norm_bwd": (ctypes.c_int, [pd] + [_P] * 10),
         "dmoe_layer_norm_workspace_bytes": (ctypes.c_size_t, [pd]),
+        "dmoe_layer_few_fwd": (ctypes.c_int, [pd] + [_P] * 14),
+        "dmoe_layer_few_workspace_bytes": (ctypes.c_size_t, [pd]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -269,6 +274,16 @@ def dmoe_layer_norm_bwd(dims, s, stats, gamma, dy, dres, dx, dgamma, dbeta, ws, 
     _check(load().dmoe_layer_norm_bwd(ctypes.byref(dims), _ptr(s), _ptr(stats), _ptr(gamma), _ptr(dy), _ptr(dres),
                                       _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), _stream(stream)),
            "dmoe_layer_norm_bwd")
+
+
+def layer_few_workspace_bytes(dims):
+    return int(load().dmoe_layer_few_workspace_bytes(ctypes.byref(dims)))
+
+
+def dmoe_layer_few_fwd(dims, x, Wg, bg, alive, W1, b1, W2, b2, res, idx, w, y, ws, stream=None):
+    _check(load().dmoe_layer_few_fwd(ctypes.byref(dims), _ptr(x), _ptr(Wg), _ptr(bg), _ptr(alive), _ptr(W1), _ptr(b1),
+                                     _ptr(W2), _ptr(b2), _ptr(res), _ptr(idx), _ptr(w), _ptr(y), _ptr(ws),
+                                     _stream(stream)), "dmoe_layer_few_fwd")
 
 
 class Trace:

@@ -1,0 +1,482 @@
+// The whole layer for a few tokens (serving): gate, exact TopK, the chosen experts' blocks and
+// their weighted average, res + DMoE(x), for at most 64 tokens.
+//
+// The call is bound by one read of the chosen experts' weights, so the tokens' rows are
+// brought to the weights and nothing else is written but h's activations and the pairs'
+// outputs (P H and P D values).  Launches: the gate's scores (fp64 partial sums over slices of
+// d_model, spread over the chip); the up-projection, whose blocks each choose the tokens'
+// experts for themselves (up to 8 tokens: one wave to a token; above, a launch of its own does
+// it) and group the pairs by expert; the down-projection; the weighted average.
+//
+// The products run on 16-row matrix instructions with the weights as the 16-row operand and
+// an expert's tokens as its 16 columns: lane (r = lane % 16, g = lane / 16) loads 16
+// consecutive bytes of weight row r straight into registers, no weight is read twice, and
+// the same vectors of the tokens' rows come from the caches.  A 16-row tile belongs to KS
+// waves, each a share of the contraction, so that the few tiles of a call with few pairs
+// still keep every compute unit's loads in flight.
+#include <algorithm>
+
+#include "gate_select.hpp"
+
+namespace dmoe {
+
+constexpr int FEW_T = 64;                 // most tokens
+constexpr int FEW_P = FEW_T * KMAX;       // most pairs
+constexpr int FEW_NT = 512, FEW_NW = FEW_NT / 64;
+static_assert(FEW_P == FEW_NT, "a thread to a pair");
+
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+
+// Workspace: the scores' partial sums, the plan, the activations, the pairs' outputs.
+struct FewPlan {                          // written by the up-projection's first block
+  int32_t E;                              // experts with rows
+  int32_t expert[FEW_P], off[FEW_P], n[FEW_P];   // each one's id, first row, rows
+  int32_t pos[FEW_P];                     // row of each pair, -1 for a dead one
+};
+struct FewWs {
+  size_t part, plan, a, yp, total;
+  int S;                                  // slices of d_model
+};
+static FewWs few_ws(const Shape& s) {
+  auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+  FewWs w{};
+  // a wave's slice of d_model: four loads of each operand, at most 32 slices for one token
+  // and four for 64 (every block of the up-projection adds them up)
+  const int64_t chunks = s.D * (int64_t)s.esz / 64;
+  w.S = (int)std::max<int64_t>(1, std::min<int64_t>({chunks / 4, 32, std::max<int64_t>(4, 128 / std::max<int64_t>(s.T, 1))}));
+  size_t off = 0;
+  w.part = off; off += up((size_t)w.S * s.T * s.dM * sizeof(double));
+  w.plan = off; off += up(sizeof(FewPlan));
+  w.a = off; off += up((size_t)s.P * s.H * s.esz);
+  w.yp = off; off += up((size_t)s.P * s.D * sizeof(float));
+  w.total = off;
+  return w;
+}
+
+struct FewArgs {
+  GateArgs gate;                          // idx and w: the caller's outputs
+  const double* part; int S;
+  FewPlan* plan;
+  const void* W; const void* bias;        // of this product: [N][R][K], [N][R]
+  const void* in; void* out;              // up: x, a;  down: a, pairs' outputs (fp32)
+  int R, K, P, act;
+};
+
+// ---------------------------------------------------------------- gate scores
+
+// part[sl][t][c] = the share of slice sl of d_model in the score of token t and gate column c,
+// on fp64 matrix instructions (operand layout as in the exact gate): a wave to 16 tokens, 16
+// columns and a slice.
+template <typename E>
+__global__ void __launch_bounds__(256) few_scores_kernel(GateArgs a, double* part, int CTN, int S, int units) {
+  constexpr int VEC = 16 / sizeof(E), CHUNK = 4 * VEC;
+  const int lane = threadIdx.x & 63;
+  const int u = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (u >= units) return;
+  const int sl = u % S, ct = u / S % CTN, tt = u / S / CTN;
+  const int r16 = lane & 15, g = lane >> 4;
+  const int t = tt * 16 + r16, col = ct * 16 + r16;
+  const E* xr = reinterpret_cast<const E*>(a.x) + (int64_t)min(t, a.T - 1) * a.D + g * VEC;
+  const E* wr = reinterpret_cast<const E*>(a.Wg) + (int64_t)min(col, a.dM - 1) * a.D + g * VEC;
+  const int nc = a.D / CHUNK;
+  const int c0 = nc * sl / S, c1 = nc * (sl + 1) / S;
+  f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
+  constexpr int U = 4;
+  for (int c = c0; c < c1; c += U) {
+    uint4 fx[U], fw[U];
+#pragma unroll
+    for (int p = 0; p < U; ++p)
+      if (c + p < c1) {
+        fx[p] = *reinterpret_cast<const uint4*>(xr + (int64_t)(c + p) * CHUNK);
+        fw[p] = *reinterpret_cast<const uint4*>(wr + (int64_t)(c + p) * CHUNK);
+      }
+#pragma unroll
+    for (int p = 0; p < U; ++p)
+      if (c + p < c1) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)vec_elem<E>(fw[p], j), (double)vec_elem<E>(fx[p], j), acc, 0,
+                                                     0, 0);
+      }
+  }
+  if (t >= a.T) return;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const int c = ct * 16 + 4 * v + g;
+    if (c < a.dM) part[((int64_t)sl * a.T + t) * a.dM + c] = acc[v];
+  }
+}
+
+// ---------------------------------------------------------------- choice of experts
+
+struct FewSelectLds {
+  double s64[FEW_NW][DM_MAX + 1];
+  SelectScratch scratch[FEW_NW];
+};
+
+// Tokens t0 .. t0 + 7 of the call, a wave to each: scores from the slices in order, then the
+// exact selection into a.idx, a.w (global or LDS, [token][k]).
+template <typename E, bool ALIVE>
+__device__ __forceinline__ void few_select(const GateArgs& a, const double* part, int S, int t0, FewSelectLds& q) {
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const E* bg = reinterpret_cast<const E*>(a.bg);
+  const int nt = min(FEW_NW, a.T - t0);
+  for (int i = threadIdx.x; i < nt * a.dM; i += FEW_NT) {
+    const int t = i / a.dM, c = i - t * a.dM;
+    double v = bg ? (double)ldf(bg + c) : 0.0;
+#pragma unroll 8
+    for (int sl = 0; sl < S; ++sl) v += part[((int64_t)sl * a.T + t0 + t) * a.dM + c];
+    q.s64[t][c] = v;
+  }
+  __syncthreads();
+  if (wv < nt) select_wave<ALIVE>(a, rank_tuples<ALIVE>(a), q.s64[wv], q.scratch[wv], t0 + wv);
+}
+
+template <typename E, bool ALIVE>
+__global__ void __launch_bounds__(FEW_NT) few_select_kernel(GateArgs a, const double* part, int S) {
+  __shared__ FewSelectLds q;
+  few_select<E, ALIVE>(a, part, S, blockIdx.x * FEW_NW, q);
+}
+
+// ---------------------------------------------------------------- the two products
+
+template <typename E> __device__ __forceinline__ f32x4_t few_mma(const uint4& w, const uint4& x, f32x4_t c);
+template <> __device__ __forceinline__ f32x4_t few_mma<bf16>(const uint4& w, const uint4& x, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, x), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4_t few_mma<float>(const uint4& w, const uint4& x, f32x4_t c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(vec_elem<float>(w, j), vec_elem<float>(x, j), c, 0, 0, 0);
+  return c;
+}
+
+// acc[q] += 16 weight rows x 16 rows of the tile's q-th group of rows, over chunks [c0, c1) of
+// the contraction (a chunk: 16 bytes to each of the four lane groups); the next U chunks are
+// loaded while the current ones are multiplied.
+template <typename E, int NQ, int U>
+__device__ __forceinline__ void few_tile(const E* wr, const E* const (&xr)[NQ], int c0, int c1, f32x4_t (&acc)[NQ]) {
+  constexpr int CHUNK = 64 / sizeof(E);
+  uint4 w[U], x[NQ][U], wn[U], xn[NQ][U];
+  auto load = [&](uint4 (&fw)[U], uint4 (&fx)[NQ][U], int c) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c + u < c1) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) fx[q][u] = *reinterpret_cast<const uint4*>(xr[q] + (int64_t)(c + u) * CHUNK);
+        fw[u] = *reinterpret_cast<const uint4*>(wr + (int64_t)(c + u) * CHUNK);
+      }
+  };
+  load(w, x, c0);
+  for (int c = c0; c < c1; c += U) {
+    load(wn, xn, c + U);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c + u < c1) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) acc[q] = few_mma<E>(w[u], x[q][u], acc[q]);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      w[u] = wn[u];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) x[q][u] = xn[q][u];
+    }
+  }
+}
+
+struct FewPlanLds {
+  __align__(16) int eid[FEW_P];          // expert of each pair, -1 for a dead one
+  __align__(16) int lead[FEW_P];         // first pair with the same expert
+  int rowpair[FEW_P];                    // pair of each row
+  int expert[FEW_P], off[FEW_P], n[FEW_P];
+};
+
+// Groups the pairs by expert (experts by their first pair, an expert's pairs in order): a thread
+// to a pair, which counts over the others.  Returns the number of experts with rows.
+__device__ __forceinline__ int few_plan(FewPlanLds& q, int P, FewPlan* out) {
+  const int p = threadIdx.x;
+  const int P4 = (P + 3) & ~3;
+  const int e = p < P4 ? q.eid[p] : -1;              // padded with -1
+  int before = 0, total = 0, lead = 1 << 20;
+  if (e >= 0)
+    for (int o = P4 - 4; o >= 0; o -= 4) {
+      const int4 v = *reinterpret_cast<const int4*>(q.eid + o);
+      const int same[4] = {v.x == e, v.y == e, v.z == e, v.w == e};
+#pragma unroll
+      for (int j = 3; j >= 0; --j) {
+        before += same[j] & (o + j < p);
+        total += same[j];
+        lead = same[j] ? o + j : lead;
+      }
+    }
+  if (p < P4) q.lead[p] = lead;
+  const int E = __syncthreads_count(e >= 0 && lead == p);
+  if (e >= 0) {
+    int slot = 0, base = 0;
+    for (int o = 0; o < P4; o += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(q.lead + o);
+      const int l[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        base += l[j] < lead;
+        slot += (l[j] < lead) & (l[j] == o + j);
+      }
+    }
+    q.rowpair[base + before] = p;
+    if (lead == p) {
+      q.expert[slot] = e; q.off[slot] = base; q.n[slot] = total;
+      if (out) { out->expert[slot] = e; out->off[slot] = base; out->n[slot] = total; }
+    }
+    if (out) out->pos[p] = base + before;
+  } else if (out && p < P) {
+    out->pos[p] = -1;
+  }
+  if (out && p == 0) out->E = E;
+  __syncthreads();
+  return E;
+}
+
+// UP: a[row] = act(W1_e x[token of row] + b1_e), and before it the choice of experts (INLINE: the
+// call has at most 8 tokens and no launch of its own chose them) and the plan.
+// Down: out[row] = W2_e a[row] + b2_e, fp32.
+// MAXQ: groups of 16 rows an expert may have (1 or 4).
+template <typename E, bool UP, bool INLINE, bool ALIVE, int KS, int MAXQ>
+__global__ void __launch_bounds__(FEW_NT) few_product_kernel(FewArgs a) {
+  constexpr int VEC = 16 / sizeof(E), CHUNK = 4 * VEC, TPB = FEW_NW / KS;
+  struct Lds {
+    union { FewSelectLds sel; f32x4_t red[FEW_NW][MAXQ][64]; };
+    FewPlanLds plan;
+  };
+  __shared__ Lds q;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, g = lane >> 4;
+  int EX;
+  if constexpr (UP) {
+    const int k = a.gate.k, p = threadIdx.x;
+    int e = -1;
+    if constexpr (INLINE) {
+      GateArgs ga = a.gate;
+      // up to 64 pairs: the choice goes to the plan's arrays first
+      ga.idx = q.plan.expert;
+      ga.w = reinterpret_cast<float*>(q.plan.off);
+      few_select<E, ALIVE>(ga, a.part, a.S, 0, q.sel);
+      __syncthreads();
+      if (p < a.P) {
+        e = q.plan.expert[p];
+        if (blockIdx.x == 0) { a.gate.idx[p] = e; a.gate.w[p] = reinterpret_cast<float*>(q.plan.off)[p]; }
+      }
+    } else {
+      if (p < a.P) e = a.gate.idx[p];
+    }
+    if (e >= 0 && a.gate.alive && !a.gate.alive[e]) e = -1;
+    q.plan.eid[p] = e;
+    __syncthreads();
+    EX = few_plan(q.plan, a.P, blockIdx.x == 0 ? a.plan : nullptr);
+    (void)k;
+  } else {
+    EX = a.plan->E;
+    const int p = threadIdx.x;
+    if (p < EX) { q.plan.expert[p] = a.plan->expert[p]; q.plan.off[p] = a.plan->off[p]; q.plan.n[p] = a.plan->n[p]; }
+    __syncthreads();
+  }
+
+  const int RT = a.R / 16, tiles = EX * RT;
+  const int ks = wv % KS, nc = a.K / CHUNK;
+  const int c0 = nc * ks / KS, c1 = nc * (ks + 1) / KS;
+  const E* in = reinterpret_cast<const E*>(a.in);
+  for (int L0 = blockIdx.x * TPB; L0 < tiles; L0 += gridDim.x * TPB) {
+    const int L = L0 + wv / KS;
+    const bool on = L < tiles;
+    f32x4_t acc[MAXQ];
+#pragma unroll
+    for (int i = 0; i < MAXQ; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    int slot = 0, e = 0, off = 0, n = 0, r0 = 0;
+    if (on) {
+      slot = L / RT;
+      r0 = (L - slot * RT) * 16;
+      e = __builtin_amdgcn_readfirstlane(q.plan.expert[slot]);
+      off = __builtin_amdgcn_readfirstlane(q.plan.off[slot]);
+      n = __builtin_amdgcn_readfirstlane(q.plan.n[slot]);
+      const E* wr = reinterpret_cast<const E*>(a.W) + ((int64_t)e * a.R + r0 + r16) * a.K + g * VEC;
+      auto row = [&](int i) {              // the operand row of the expert's i-th row (the last one past its end)
+        const int r = off + min(i, n - 1);
+        return in + (int64_t)(UP ? q.plan.rowpair[r] / a.gate.k : r) * a.K + g * VEC;
+      };
+      if (MAXQ == 1 || n <= 16) {
+        const E* xr[1] = {row(r16)};
+        few_tile<E, 1, 8>(wr, xr, c0, c1, reinterpret_cast<f32x4_t(&)[1]>(acc));
+      } else if constexpr (MAXQ == 4) {
+        if (n <= 32) {
+          const E* xr[2] = {row(r16), row(16 + r16)};
+          few_tile<E, 2, 4>(wr, xr, c0, c1, reinterpret_cast<f32x4_t(&)[2]>(acc));
+        } else {
+          const E* xr[4] = {row(r16), row(16 + r16), row(32 + r16), row(48 + r16)};
+          few_tile<E, 4, 4>(wr, xr, c0, c1, acc);
+        }
+      }
+    }
+    if constexpr (KS > 1) {
+      // the tile's waves, added in order
+      if (ks)
+#pragma unroll
+        for (int i = 0; i < MAXQ; ++i) q.red[wv][i][lane] = acc[i];
+      __syncthreads();
+      if (ks == 0)
+#pragma unroll
+        for (int w = 1; w < KS; ++w)
+#pragma unroll
+          for (int i = 0; i < MAXQ; ++i) acc[i] += q.red[wv + w][i][lane];
+    }
+    if (on && ks == 0) {
+      // lane: weight rows r0 + 4 g .. + 3 of its row
+      const int c = r0 + 4 * g;
+      const E* bp = reinterpret_cast<const E*>(a.bias) + (int64_t)e * a.R + c;
+      float b[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = ldf(bp + j);
+#pragma unroll
+      for (int i = 0; i < MAXQ; ++i) {
+        const int r = 16 * i + r16;
+        if (r >= n) continue;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = acc[i][j] + b[j];
+        if constexpr (UP) {
+          // the activation is rounded to the layer's type, the matrix operand of the next product
+          E* o = reinterpret_cast<E*>(a.out) + (int64_t)(off + r) * a.R + c;
+          if constexpr (sizeof(E) == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = act_fwd_fast(v[j], a.act);
+            *reinterpret_cast<uint2*>(o) = make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = act_fwd(v[j], a.act);
+            *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+          }
+        } else {
+          float* o = reinterpret_cast<float*>(a.out) + (int64_t)(off + r) * a.R + c;
+          *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+      }
+    }
+    if constexpr (KS > 1) __syncthreads();
+  }
+}
+
+// y[t] = res[t] + sum_j w[t,j] out[pos[t,j]], in slot order, one rounding
+template <typename E>
+__global__ void __launch_bounds__(256)
+few_combine_kernel(const FewPlan* plan, const float* yp, const float* w, const E* res, E* y, int D, int k) {
+  constexpr int VEC = Vec<E>::N;
+  const int t = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * VEC;
+  if (c >= D) return;
+  float o[VEC];
+  if (res) Vec<E>::unpack(*reinterpret_cast<const uint4*>(res + (int64_t)t * D + c), o);
+  else
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) o[j] = 0.f;
+  float s[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) s[j] = 0.f;
+  for (int i = 0; i < k; ++i) {
+    const int p = plan->pos[t * k + i];
+    if (p < 0) continue;
+    const float wi = w[t * k + i];
+#pragma unroll
+    for (int j = 0; j < VEC; j += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(yp + (int64_t)p * D + c + j);
+      s[j] = fmaf(wi, v.x, s[j]); s[j + 1] = fmaf(wi, v.y, s[j + 1]);
+      s[j + 2] = fmaf(wi, v.z, s[j + 2]); s[j + 3] = fmaf(wi, v.w, s[j + 3]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) o[j] += s[j];
+  *reinterpret_cast<uint4*>(y + (int64_t)t * D + c) = Vec<E>::pack(o);
+}
+
+// ---------------------------------------------------------------- host
+
+// Waves to a tile: enough for eight waves a compute unit, each at least four chunks of the
+// contraction.
+static int few_split(const Shape& s, int64_t R, int64_t K) {
+  const int64_t tiles = std::min(s.P, s.N) * (R / 16), chunks = K * (int64_t)s.esz / 64;
+  int ks = 1;
+  while (ks < FEW_NW && tiles * ks < 2048 && chunks / (2 * ks) >= 4) ks *= 2;
+  return ks;
+}
+
+template <typename E, bool UP, bool INLINE, bool ALIVE>
+static void few_product(const Shape& s, const FewArgs& a, hipStream_t st) {
+  const int ks = few_split(s, a.R, a.K);
+  const int64_t tiles = std::min(s.P, s.N) * (a.R / 16), tpb = FEW_NW / ks;
+  const dim3 grid((unsigned)std::min<int64_t>((tiles + tpb - 1) / tpb, 512));
+  auto go = [&](auto KSc) {
+    constexpr int KS = decltype(KSc)::value;
+    if (ks != KS) return;
+    auto kern = s.T <= 16 || INLINE ? few_product_kernel<E, UP, INLINE, ALIVE, KS, 1>
+                                    : few_product_kernel<E, UP, INLINE, ALIVE, KS, INLINE ? 1 : 4>;
+    DMOE_LAUNCH_NAMED(UP ? "few_product_kernel (up)" : "few_product_kernel (down)", kern, grid, dim3(FEW_NT), 0, st, a);
+  };
+  go(std::integral_constant<int, 1>{});
+  go(std::integral_constant<int, 2>{});
+  go(std::integral_constant<int, 4>{});
+  go(std::integral_constant<int, 8>{});
+}
+
+template <typename E>
+static void layer_few_fwd(const Shape& s, const GateArgs& g, const void* W1, const void* b1, const void* W2, const void* b2,
+                          const void* res, void* y, unsigned char* ws, hipStream_t st) {
+  const FewWs L = few_ws(s);
+  double* part = reinterpret_cast<double*>(ws + L.part);
+  FewPlan* plan = reinterpret_cast<FewPlan*>(ws + L.plan);
+  const bool alive_first = (s.flags & DMOE_FLAG_ALIVE_TOPK) != 0;
+  const int CTN = (int)((s.dM + 15) / 16), units = (int)((s.T + 15) / 16) * CTN * L.S;
+  DMOE_LAUNCH_NAMED("few_scores_kernel", few_scores_kernel<E>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, g, part,
+                    CTN, L.S, units);
+  const bool inl = s.T <= FEW_NW;
+  if (!inl) {
+    auto kern = alive_first ? few_select_kernel<E, true> : few_select_kernel<E, false>;
+    DMOE_LAUNCH_NAMED("few_select_kernel", kern, dim3((unsigned)((s.T + FEW_NW - 1) / FEW_NW)), dim3(FEW_NT), 0, st, g, part,
+                      L.S);
+  }
+  FewArgs up{g, part, L.S, plan, W1, b1, g.x, ws + L.a, (int)s.H, (int)s.D, (int)s.P, s.act};
+  if (!inl) few_product<E, true, false, false>(s, up, st);
+  else if (alive_first) few_product<E, true, true, true>(s, up, st);
+  else few_product<E, true, true, false>(s, up, st);
+  FewArgs down{g, part, L.S, plan, W2, b2, ws + L.a, ws + L.yp, (int)s.D, (int)s.H, (int)s.P, s.act};
+  few_product<E, false, false, false>(s, down, st);
+  const int cols = 256 * Vec<E>::N;
+  DMOE_LAUNCH_NAMED("few_combine_kernel", few_combine_kernel<E>, dim3((unsigned)((s.D + cols - 1) / cols), (unsigned)s.T),
+                    dim3(256), 0, st, plan, reinterpret_cast<const float*>(ws + L.yp), g.w, reinterpret_cast<const E*>(res),
+                    reinterpret_cast<E*>(y), (int)s.D, s.k);
+}
+
+}  // namespace dmoe
+
+using namespace dmoe;
+
+extern "C" size_t dmoe_layer_few_workspace_bytes(const dmoe_dims* dims) {
+  Shape s;
+  if (check_dims(dims, &s) != DMOE_OK || s.T > FEW_T) return 0;
+  return few_ws(s).total;
+}
+
+extern "C" int dmoe_layer_few_fwd(const dmoe_dims* dims, const void* x, const void* Wg, const void* bg, const uint8_t* alive,
+                                  const void* W1, const void* b1, const void* W2, const void* b2, const void* res,
+                                  int32_t* idx, float* w, void* y, void* ws, void* stream) {
+  Shape s;
+  int rc = check_dims(dims, &s);
+  if (rc) return rc;
+  if (s.T > FEW_T) return DMOE_EUNSUPPORTED;
+  if (s.T == 0) return DMOE_OK;
+  if (!x || !Wg || !W1 || !b1 || !W2 || !b2 || !idx || !w || !y || !ws) return DMOE_EINVAL;
+  for (const void* q : {x, Wg, W1, b1, W2, b2, res, (const void*)y, (const void*)ws})
+    if (!aligned16(q)) return DMOE_EUNSUPPORTED;
+  const GateArgs g{x, Wg, bg, alive, idx, w, nullptr, nullptr, (int)s.T, (int)s.D, s.d, s.M, s.k, (int)s.dM, (int)s.N};
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  unsigned char* base = reinterpret_cast<unsigned char*>(ws);
+  if (s.dtype == DMOE_BF16) layer_few_fwd<bf16>(s, g, W1, b1, W2, b2, res, y, base, st);
+  else layer_few_fwd<float>(s, g, W1, b1, W2, b2, res, y, base, st);
+  return launch_status();
+}

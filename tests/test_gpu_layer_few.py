@@ -1,0 +1,256 @@
+"""The whole layer for a few tokens against the definition in 64 bits: the choice of experts
+exactly, weights and outputs within bounds added up operation by operation (u = 2^-24 per
+fp32 operation; the activations and the result rounded to the layer's type, half a step)."""
+import numpy as np
+import pytest
+import torch
+from scipy.special import erf
+
+import oracle as O
+from paper_2002_04013_amd import abi
+from parity_util import say
+
+U = 2.0 ** -24
+
+
+def _inputs(T, D, H, d, M, k, dtype, seed, p_alive=1.0):
+    g = torch.Generator().manual_seed(seed)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    r = lambda *s, sc=1.0: (torch.randn(*s, generator=g) * sc).to(dt)
+    N = M ** d
+    return dict(x=r(T, D), Wg=r(d * M, D, sc=D ** -0.5), bg=r(d * M, sc=0.1), W1=r(N, H, D, sc=D ** -0.5), b1=r(N, H),
+                W2=r(N, D, H, sc=H ** -0.5), b2=r(N, D), res=r(T, D),
+                alive=(torch.rand(N, generator=g) < p_alive).to(torch.uint8))
+
+
+def _reference(q, T, d, M, k, dtype, act, alive_topk, bg=True, alive=True, res=True):
+    """idx, w, y and the bound on y's error."""
+    f = {n: O.to64(v) for n, v in q.items() if n != "alive"}
+    live = q["alive"].numpy().astype(bool) if alive else np.ones(M ** d, bool)
+    S = O.gate_scores(f["x"], f["Wg"], f["bg"] if bg else None)
+    S32 = O.decision_scores(S)
+    idx = (O.topk_alive_bruteforce(S32, d, M, k, live) if alive_topk else O.topk_bruteforce(S32, d, M, k))[0]
+    gx = np.zeros(idx.shape)
+    for i in range(d):
+        gx += np.take_along_axis(S, (idx // M ** (d - 1 - i)) % M + i * M, axis=1)
+    on = live[idx]
+    e = np.exp(np.where(on, gx - np.where(on, gx, -np.inf).max(1, initial=-1e300, keepdims=True), -np.inf))
+    den = e.sum(1, keepdims=True)
+    w = np.divide(e, den, out=np.zeros_like(e), where=den > 0)
+    half = torch.finfo(torch.bfloat16).eps / 2 if dtype == "bf16" else U
+    D, H = f["x"].shape[1], f["W1"].shape[1]
+    y = f["res"].copy() if res else np.zeros_like(f["x"])
+    err = U * np.abs(y)
+    for t in range(T):
+        for j in range(k):
+            if not on[t, j]:
+                continue
+            n = idx[t, j]
+            W1, W2 = f["W1"][n], f["W2"][n]
+            h = W1 @ f["x"][t] + f["b1"][n]
+            eh = (D + 2) * U * (np.abs(W1) @ np.abs(f["x"][t]) + np.abs(f["b1"][n]))
+            # |gelu'| <= 1.13; the activation itself to 3e-5 of |h| in bf16 layers (see its comment), 8 u in fp32 ones
+            a = np.maximum(h, 0) if act == "relu" else 0.5 * h * (1 + erf(h / np.sqrt(2)))
+            ea = 1.13 * eh + (3e-5 if dtype == "bf16" else 8 * U) * np.abs(h)
+            ea = ea + half * (np.abs(a) + ea)
+            o = W2 @ a + f["b2"][n]
+            eo = np.abs(W2) @ ea + (H + 2) * U * (np.abs(W2) @ (np.abs(a) + ea) + np.abs(f["b2"][n]))
+            y[t] += w[t, j] * o
+            err[t] += w[t, j] * (eo + (16 + 4 * np.abs(gx[t]).max()) * U * np.abs(o))
+    return idx, w, y, err + half * (np.abs(y) + err) + 2 * U * np.abs(y)
+
+
+def _run(q, T, D, H, d, M, k, dtype, act, alive_topk=False, bg=True, alive=True, res=True, ws=None):
+    t = {n: v.cuda() for n, v in q.items()}
+    dims = abi.make_dims(T, D, H, d, M, k, dtype, act, abi.DMOE_FLAG_ALIVE_TOPK if alive_topk else 0)
+    idx = torch.full((T, k), -7, dtype=torch.int32, device="cuda")
+    w = torch.full((T, k), float("nan"), device="cuda")
+    y = torch.full_like(t["x"], float("nan"))
+    if ws is None:
+        ws = torch.full((abi.layer_few_workspace_bytes(dims),), 255, dtype=torch.uint8, device="cuda")
+    abi.dmoe_layer_few_fwd(dims, t["x"], t["Wg"], t["bg"] if bg else None, t["alive"] if alive else None, t["W1"], t["b1"],
+                           t["W2"], t["b2"], t["res"] if res else None, idx, w, y, ws)
+    torch.cuda.synchronize()
+    return idx.cpu().numpy(), O.to64(w), O.to64(y)
+
+
+def _check(name, T, D, H, d, M, k, dtype, act, p_alive=1.0, alive_topk=False, **kw):
+    say(f"[few] {name}")
+    q = _inputs(T, D, H, d, M, k, dtype, sum(map(ord, name)), p_alive)
+    if p_alive == 0.0:
+        q["alive"].zero_()
+    idx, w, y = _run(q, T, D, H, d, M, k, dtype, act, alive_topk, **kw)
+    ridx, rw, ry, bound = _reference(q, T, d, M, k, dtype, act, alive_topk, **kw)
+    assert np.array_equal(idx, ridx)
+    assert (np.abs(w - rw) <= (16 + 64) * U * rw).all()
+    worst = np.max(np.abs(y - ry) / np.maximum(bound, 1e-300))
+    assert worst <= 1.0, f"y: {worst:.3g} of the bound"
+
+
+CASES = [
+    # tokens at the borders of the launches' forms (8, 16, 32, 64), few experts so that one has all of them
+    ("one token", 1, 64, 64, 1, 2, 1), ("three", 3, 64, 256, 2, 4, 2), ("eight", 8, 128, 192, 2, 4, 3),
+    ("nine", 9, 128, 192, 2, 4, 3), ("sixteen rows", 16, 64, 128, 1, 2, 2), ("seventeen rows", 17, 64, 128, 1, 2, 2),
+    ("thirty-three rows", 33, 128, 64, 1, 3, 3), ("all rows", 64, 64, 192, 1, 1, 1), ("512 pairs", 64, 64, 64, 1, 8, 8),
+    ("512 pairs apart", 64, 64, 64, 2, 64, 8), ("128 gate columns", 5, 192, 64, 4, 32, 0), ("deep grid", 7, 64, 64, 4, 5, 8),
+    # contractions of every share of waves, odd numbers of chunks
+    ("long d_model", 2, 4160, 64, 1, 3, 2), ("long hidden", 2, 64, 4160, 1, 3, 2), ("wide tiles", 4, 64, 8256, 1, 2, 1),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("case", CASES, ids=[c[0].replace(" ", "_") for c in CASES])
+def test_against_definition(case, dtype, act):
+    name, T, D, H, d, M, k = case
+    if name == "128 gate columns":
+        d, M, k = 1, 128, 4
+    _check(f"{name} {dtype} {act}", T, D, H, d, M, k, dtype, act)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [2, 13, 40])
+@pytest.mark.parametrize("p_alive", [0.0, 0.15, 0.6])
+@pytest.mark.parametrize("alive_topk", [False, True])
+def test_dead_experts(T, p_alive, alive_topk, dtype):
+    """Tokens whose chosen experts are partly, or all, dead; with and without TopK among the alive ones."""
+    _check(f"dead {T} {p_alive} {alive_topk} {dtype}", T, 64, 128, 2, 5, 4, dtype, "gelu", p_alive, alive_topk)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw", [dict(bg=False), dict(alive=False), dict(res=False), dict(bg=False, alive=False, res=False)])
+def test_left_out_arguments(kw):
+    _check(f"without {sorted(kw)}", 5, 128, 128, 2, 3, 2, "bf16", "gelu", 0.7, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [4, 20])
+def test_equal_scores_go_to_the_lower_index(T):
+    """A gate of equal rows: every cell has the same total, the k first flat indices are chosen."""
+    q = _inputs(T, 64, 64, 2, 4, 3, "bf16", 3)
+    q["Wg"][:] = q["Wg"][0]
+    q["bg"][:] = 0
+    idx, w, _ = _run(q, T, 64, 64, 2, 4, 3, "bf16", "relu")
+    assert (idx == np.arange(3)).all() and np.abs(w - 1 / 3).max() < 4 * U
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 30])
+def test_against_the_layer_and_over_inputs(T):
+    """The regular layer's choice and outputs (bf16: its h, a and expert outputs rounded once more each); y over x or
+    res; a token alone as among others."""
+    from paper_2002_04013_amd import DMoELayer
+    D, H, d, M, k = 256, 512, 2, 6, 4
+    q = _inputs(T, D, H, d, M, k, "bf16", 11, 0.8)
+    t = {n: v.cuda() for n, v in q.items()}
+    L = DMoELayer(T, D, H, d, M, k, "bf16", "gelu")
+    ref = L.forward(t["x"], t["Wg"], t["bg"], t["alive"], t["W1"], t["b1"], t["W2"], t["b2"]).double()
+    dims = L.dims
+    ws = torch.empty(abi.layer_few_workspace_bytes(dims), dtype=torch.uint8, device="cuda")
+    idx, w, y = torch.empty_like(L.idx), torch.empty_like(L.w), torch.empty_like(t["x"])
+    args = lambda x, res, y: (dims, x, t["Wg"], t["bg"], t["alive"], t["W1"], t["b1"], t["W2"], t["b2"], res, idx, w, y, ws)
+    abi.dmoe_layer_few_fwd(*args(t["x"], None, y))
+    assert torch.equal(idx, L.idx)
+    # roundings: h, a, the experts' outputs and y there, a and y here, each 2^-8 of values of order one
+    assert (y.double() - ref).abs().max() <= 6 * 2.0 ** -8 * ref.abs().max()
+    with_res = torch.empty_like(y)
+    abi.dmoe_layer_few_fwd(*args(t["x"], t["res"], with_res))
+    for over in ("x", "res"):
+        c = {"x": t["x"].clone(), "res": t["res"].clone()}
+        abi.dmoe_layer_few_fwd(*args(c["x"], c["res"], c[over]))
+        assert torch.equal(c[over], with_res)
+    one = abi.make_dims(1, D, H, d, M, k, "bf16", "gelu")
+    for i in (0, T - 1):
+        i1, w1, y1 = torch.empty_like(idx[:1]), torch.empty_like(w[:1]), torch.empty_like(y[:1])
+        abi.dmoe_layer_few_fwd(one, t["x"][i:i + 1].clone(), t["Wg"], t["bg"], t["alive"], t["W1"], t["b1"], t["W2"],
+                               t["b2"], None, i1, w1, y1, ws)
+        assert torch.equal(i1, idx[i:i + 1])
+        # the same products in another order of sums
+        assert (y1.double() - y[i:i + 1].double()).abs().max() <= 2.0 ** -7 * y.double().abs().max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 23])
+def test_streams_and_graph_replay(T):
+    """Two streams with a workspace each at once, and a captured call replayed over junk: the eager call, bit for bit."""
+    D, H, d, M, k = 128, 256, 2, 4, 3
+    q = _inputs(T, D, H, d, M, k, "bf16", 21, 0.9)
+    t = {n: v.cuda() for n, v in q.items()}
+    dims = abi.make_dims(T, D, H, d, M, k, "bf16", "gelu")
+
+    def buffers():
+        return (torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda"),
+                torch.empty_like(t["x"]), torch.empty(abi.layer_few_workspace_bytes(dims), dtype=torch.uint8, device="cuda"))
+
+    def call(b, x, stream=None):
+        abi.dmoe_layer_few_fwd(dims, x, t["Wg"], t["bg"], t["alive"], t["W1"], t["b1"], t["W2"], t["b2"], t["res"], *b,
+                               stream=stream)
+
+    x2 = t["x"].flip(0).contiguous()
+    a, b, ra, rb = (buffers() for _ in range(4))
+    call(ra, t["x"])
+    call(rb, x2)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        call(a, t["x"], s1)
+        call(b, x2, s2)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, r) for p, r in zip(a[:3] + b[:3], ra[:3] + rb[:3]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(a, t["x"])
+    for _ in range(3):
+        for v in a:
+            v.fill_(77)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, r) for p, r in zip(a[:3], ra[:3]))
+
+
+@pytest.mark.gpu
+def test_large_stack_offsets():
+    """Experts past 4 GiB of weights: the last of a stack whose element offsets pass 2^31."""
+    T, D, H, N, k = 2, 1024, 4096, 520, 1
+    t = {n: v.cuda() for n, v in _inputs(T, D, H, 1, 1, 1, "bf16", 31).items()}
+    W1 = torch.zeros(N, H, D, dtype=torch.bfloat16, device="cuda")
+    W2 = torch.zeros(N, D, H, dtype=torch.bfloat16, device="cuda")
+    b1, b2 = torch.zeros(N, H, dtype=torch.bfloat16, device="cuda"), torch.zeros(N, D, dtype=torch.bfloat16, device="cuda")
+    W1[-1], W2[-1], b1[-1], b2[-1] = t["W1"][0], t["W2"][0], t["b1"][0], t["b2"][0]
+    # a 3-D grid of 8 x 8 x 8 has 512 cells; 520 = 65 * 8 needs a grid of its own: one dimension of 128 does not hold it,
+    # so the grid is 23 x 23 = 529 cells with the cells past the stack dead
+    M = 23
+    alive = torch.zeros(M * M, dtype=torch.uint8, device="cuda")
+    alive[N - 1] = 1
+    pad = lambda w: torch.cat((w, w.new_zeros(M * M - N, *w.shape[1:])))
+    Wg = torch.zeros(2 * M, D, dtype=torch.bfloat16, device="cuda")
+    dims = abi.make_dims(T, D, H, 2, M, k, "bf16", "gelu", abi.DMOE_FLAG_ALIVE_TOPK)
+    out = [torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda"), torch.empty_like(t["x"]),
+           torch.empty(abi.layer_few_workspace_bytes(dims), dtype=torch.uint8, device="cuda")]
+    abi.dmoe_layer_few_fwd(dims, t["x"], Wg, None, alive, pad(W1), pad(b1), pad(W2), pad(b2), None, *out)
+    one = abi.make_dims(T, D, H, 1, 1, 1, "bf16", "gelu")
+    ref = [torch.empty_like(v) for v in out[:3]]
+    abi.dmoe_layer_few_fwd(one, t["x"], Wg[:1].contiguous(), None, None, t["W1"], t["b1"], t["W2"], t["b2"], None, *ref, out[3])
+    assert (out[0] == N - 1).all() and (out[1] == 1).all()
+    assert (out[2].double() - ref[2].double()).abs().max() <= 2.0 ** -7 * ref[2].double().abs().max()
+
+
+@pytest.mark.parametrize("what,rc", [
+    ("no tokens", 0), ("x", -1), ("Wg", -1), ("W1", -1), ("b1", -1), ("W2", -1), ("b2", -1), ("idx", -1), ("w", -1), ("y", -1),
+    ("ws", -1), ("W2 off by 8 bytes", -2), ("ws off by 4 bytes", -2), ("65 tokens", -2), ("k > N", -1)])
+def test_refusals_on_host(what, rc):
+    names = ("x", "Wg", "bg", "alive", "W1", "b1", "W2", "b2", "res", "idx", "w", "y", "ws")
+    a = {n: abi.ctypes.c_void_p((i + 1) << 20) for i, n in enumerate(names)}
+    if what in a:
+        a[what] = None
+    if "off by" in what:
+        n, off = what.split()[0], int(what.split()[3])
+        a[n] = abi.ctypes.c_void_p((1 << 24) + off)
+    T = {"no tokens": 0, "65 tokens": 65}.get(what, 8)
+    dims = abi.make_dims(T, 64, 64, 1, 4, 5 if what == "k > N" else 2, "bf16", "relu")
+    assert abi.load().dmoe_layer_few_fwd(abi.ctypes.byref(dims), *a.values(), None) == rc
+    if what in ("65 tokens", "k > N"):
+        assert abi.layer_few_workspace_bytes(dims) == 0
