@@ -9,9 +9,8 @@
 // it) and group the pairs by expert; the down-projection; the weighted average.
 //
 // The products run on 16-row matrix instructions with the weights as the 16-row operand and
-// an expert's tokens as its 16 columns: lane (r = lane % 16, g = lane / 16) loads 16
-// consecutive bytes of weight row r straight into registers, no weight is read twice, and
-// the same vectors of the tokens' rows come from the caches.  A 16-row tile belongs to KS
+// an expert's tokens as its 16 columns; no weight is read twice, and the vectors of the
+// tokens' rows come from the caches.  A 16-row tile belongs to KS
 // waves, each a share of the contraction, so that the few tiles of a call with few pairs
 // still keep every compute unit's loads in flight.
 #include <algorithm>
@@ -22,10 +21,15 @@ namespace dmoe {
 
 constexpr int FEW_T = 64;                 // most tokens
 constexpr int FEW_P = FEW_T * KMAX;       // most pairs
+// largest T d M D of scores that the up-projection's blocks compute themselves.  Own launch / in the
+// blocks: T = 1, 8192 values (fp32, D = 64) 18.3 / 15.2 us a call; T = 1, 32 columns, D = 1024
+// 24.3 / 22.4; T = 1, 64 columns, D = 1024 29.4 / 29.7; T = 4 of them 70.5 / 82.6.
+constexpr int64_t FEW_INLINE = 32768;
 constexpr int FEW_NT = 512, FEW_NW = FEW_NT / 64;
 static_assert(FEW_P == FEW_NT, "a thread to a pair");
 
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // Workspace: the scores' partial sums, the plan, the activations, the pairs' outputs.
 struct FewPlan {                          // written by the up-projection's first block
@@ -55,7 +59,7 @@ static FewWs few_ws(const Shape& s) {
 
 struct FewArgs {
   GateArgs gate;                          // idx and w: the caller's outputs
-  const double* part; int S;
+  const double* part; int S;              // part NULL: the up-projection's blocks do the scores
   FewPlan* plan;
   const void* W; const void* bias;        // of this product: [N][R][K], [N][R]
   const void* in; void* out;              // up: x, a;  down: a, pairs' outputs (fp32)
@@ -114,22 +118,65 @@ struct FewSelectLds {
   SelectScratch scratch[FEW_NW];
 };
 
-// Tokens t0 .. t0 + 7 of the call, a wave to each: scores from the slices in order, then the
-// exact selection into a.idx, a.w (global or LDS, [token][k]).
+// Tokens t0 .. t0 + 7 of the call, a wave to each: scores from the slices in order (part NULL:
+// they are in q already), then the exact selection into a.idx, a.w (global or LDS, [token][k]).
 template <typename E, bool ALIVE>
 __device__ __forceinline__ void few_select(const GateArgs& a, const double* part, int S, int t0, FewSelectLds& q) {
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const E* bg = reinterpret_cast<const E*>(a.bg);
   const int nt = min(FEW_NW, a.T - t0);
-  for (int i = threadIdx.x; i < nt * a.dM; i += FEW_NT) {
-    const int t = i / a.dM, c = i - t * a.dM;
-    double v = bg ? (double)ldf(bg + c) : 0.0;
+  const RankTuples tup = rank_tuples<ALIVE>(a);      // loaded while the scores are summed
+  if (part)
+    for (int i = threadIdx.x; i < nt * a.dM; i += FEW_NT) {
+      const int t = i / a.dM, c = i - t * a.dM;
+      double v = bg ? (double)ldf(bg + c) : 0.0;
 #pragma unroll 8
-    for (int sl = 0; sl < S; ++sl) v += part[((int64_t)sl * a.T + t0 + t) * a.dM + c];
-    q.s64[t][c] = v;
+      for (int sl = 0; sl < S; ++sl) v += part[((int64_t)sl * a.T + t0 + t) * a.dM + c];
+      q.s64[t][c] = v;
+    }
+  __syncthreads();
+  if (wv < nt) select_wave<ALIVE>(a, tup, q.s64[wv], q.scratch[wv], t0 + wv);
+}
+
+// The scores of all tokens by one block, for calls with so few products (FEW_INLINE) that every
+// block of the up-projection does them sooner than a launch of its own: a wave to four
+// columns of a token, its lanes along d_model, fp64 multiply-adds of the exact values.
+template <typename E>
+__device__ __forceinline__ void few_scores_block(const GateArgs& a, FewSelectLds& q) {
+  constexpr int VEC = 16 / sizeof(E), C = 4;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const E* bg = reinterpret_cast<const E*>(a.bg);
+  const E* Wg = reinterpret_cast<const E*>(a.Wg);
+  const int nv = a.D / VEC, groups = (a.dM + C - 1) / C;
+  for (int u = wv; u < a.T * groups; u += FEW_NW) {
+    const int t = u / groups, c0 = (u - t * groups) * C;
+    const E* xr = reinterpret_cast<const E*>(a.x) + (int64_t)t * a.D;
+    double acc[C] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 2
+    for (int v = lane; v < nv; v += 64) {
+      const uint4 fx = *reinterpret_cast<const uint4*>(xr + v * VEC);
+      uint4 fw[C];
+#pragma unroll
+      for (int i = 0; i < C; ++i)
+        fw[i] = *reinterpret_cast<const uint4*>(Wg + (int64_t)min(c0 + i, a.dM - 1) * a.D + v * VEC);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const double xj = (double)vec_elem<E>(fx, j);
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[i] = fma(xj, (double)vec_elem<E>(fw[i], j), acc[i]);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < C; ++i) acc[i] += __shfl_xor(acc[i], o, WAVE);
+    if (lane < C && c0 + lane < a.dM) {
+      const int c = c0 + lane;
+      const double v = lane == 0 ? acc[0] : lane == 1 ? acc[1] : lane == 2 ? acc[2] : acc[3];
+      q.s64[t][c] = v + (bg ? (double)ldf(bg + c) : 0.0);
+    }
   }
   __syncthreads();
-  if (wv < nt) select_wave<ALIVE>(a, rank_tuples<ALIVE>(a), q.s64[wv], q.scratch[wv], t0 + wv);
 }
 
 template <typename E, bool ALIVE>
@@ -152,36 +199,49 @@ template <> __device__ __forceinline__ f32x4_t few_mma<float>(const uint4& w, co
 }
 
 // acc[q] += 16 weight rows x 16 rows of the tile's q-th group of rows, over chunks [c0, c1) of
-// the contraction (a chunk: 16 bytes to each of the four lane groups); the next U chunks are
-// loaded while the current ones are multiplied.
+// the contraction (a chunk: 64 bytes of a row, 16 to each lane group).  U chunks a step, the next
+// step's loaded while the current ones are multiplied.  A load instruction takes 64 U contiguous
+// bytes of each of 16 / U weight rows and the wave's own piece of LDS (16 rows of 64 U + 16 bytes)
+// turns them into operands: lanes that each load 16 bytes of a row of their own, as the operands
+// want them, touch 16 cache lines per 16 lanes.
 template <typename E, int NQ, int U>
-__device__ __forceinline__ void few_tile(const E* wr, const E* const (&xr)[NQ], int c0, int c1, f32x4_t (&acc)[NQ]) {
-  constexpr int CHUNK = 64 / sizeof(E);
-  uint4 w[U], x[NQ][U], wn[U], xn[NQ][U];
-  auto load = [&](uint4 (&fw)[U], uint4 (&fx)[NQ][U], int c) {
+__device__ __forceinline__ void few_tile(const E* wt, int64_t ld, const E* const (&xr)[NQ], int c0, int c1, char* lds,
+                                         f32x4_t (&acc)[NQ]) {
+  constexpr int CHUNK = 64 / sizeof(E), RPL = 16 / U, PITCH = 64 * U + 16;
+  const int lane = threadIdx.x & 63, lr = lane / (4 * U), lu = lane % (4 * U);
+  const char* wp = reinterpret_cast<const char*>(wt + lr * ld);
+  char* wr_at = lds + lr * PITCH + lu * 16;
+  const char* rd_at = lds + (lane & 15) * PITCH + (lane >> 4) * 16;
+  uint4 x[NQ][U], xn[NQ][U];
+  u32x4_t w[U];
+  auto load = [&](uint4 (&fx)[NQ][U], u32x4_t (&fw)[U], int c) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (c + u < c1) {
+      if (c + u < c1)
 #pragma unroll
         for (int q = 0; q < NQ; ++q) fx[q][u] = *reinterpret_cast<const uint4*>(xr[q] + (int64_t)(c + u) * CHUNK);
-        fw[u] = *reinterpret_cast<const uint4*>(wr + (int64_t)(c + u) * CHUNK);
-      }
+    if (c < c1) {
+      const char* p = wp + min(4 * c + lu, 4 * c1 - 1) * 16;        // past the end: not used
+#pragma unroll
+      for (int i = 0; i < U; ++i) fw[i] = *reinterpret_cast<const u32x4_t*>(p + i * RPL * ld * (int64_t)sizeof(E));
+    }
   };
-  load(w, x, c0);
+  load(x, w, c0);
   for (int c = c0; c < c1; c += U) {
-    load(wn, xn, c + U);
+#pragma unroll
+    for (int i = 0; i < U; ++i) *reinterpret_cast<u32x4_t*>(wr_at + i * RPL * PITCH) = w[i];
+    load(xn, w, c + U);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (c + u < c1) {
+        const uint4 wf = *reinterpret_cast<const uint4*>(rd_at + u * 64);
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) acc[q] = few_mma<E>(w[u], x[q][u], acc[q]);
+        for (int q = 0; q < NQ; ++q) acc[q] = few_mma<E>(wf, x[q][u], acc[q]);
       }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      w[u] = wn[u];
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int q = 0; q < NQ; ++q) x[q][u] = xn[q][u];
-    }
   }
 }
 
@@ -245,7 +305,10 @@ template <typename E, bool UP, bool INLINE, bool ALIVE, int KS, int MAXQ>
 __global__ void __launch_bounds__(FEW_NT) few_product_kernel(FewArgs a) {
   constexpr int VEC = 16 / sizeof(E), CHUNK = 4 * VEC, TPB = FEW_NW / KS;
   struct Lds {
-    union { FewSelectLds sel; f32x4_t red[FEW_NW][MAXQ][64]; };
+    union {
+      FewSelectLds sel;
+      struct { f32x4_t red[FEW_NW][MAXQ][64]; __align__(16) char turn[FEW_NW][16 * (64 * 8 + 16)]; };
+    };
     FewPlanLds plan;
   };
   __shared__ Lds q;
@@ -253,13 +316,14 @@ __global__ void __launch_bounds__(FEW_NT) few_product_kernel(FewArgs a) {
   const int r16 = lane & 15, g = lane >> 4;
   int EX;
   if constexpr (UP) {
-    const int k = a.gate.k, p = threadIdx.x;
+    const int p = threadIdx.x;
     int e = -1;
     if constexpr (INLINE) {
       GateArgs ga = a.gate;
       // up to 64 pairs: the choice goes to the plan's arrays first
       ga.idx = q.plan.expert;
       ga.w = reinterpret_cast<float*>(q.plan.off);
+      if (!a.part) few_scores_block<E>(ga, q.sel);
       few_select<E, ALIVE>(ga, a.part, a.S, 0, q.sel);
       __syncthreads();
       if (p < a.P) {
@@ -273,11 +337,14 @@ __global__ void __launch_bounds__(FEW_NT) few_product_kernel(FewArgs a) {
     q.plan.eid[p] = e;
     __syncthreads();
     EX = few_plan(q.plan, a.P, blockIdx.x == 0 ? a.plan : nullptr);
-    (void)k;
   } else {
     EX = a.plan->E;
     const int p = threadIdx.x;
-    if (p < EX) { q.plan.expert[p] = a.plan->expert[p]; q.plan.off[p] = a.plan->off[p]; q.plan.n[p] = a.plan->n[p]; }
+    if (p < a.P) {                         // those past the last expert are not used
+      q.plan.expert[p] = a.plan->expert[p];
+      q.plan.off[p] = a.plan->off[p];
+      q.plan.n[p] = a.plan->n[p];
+    }
     __syncthreads();
   }
 
@@ -298,21 +365,21 @@ __global__ void __launch_bounds__(FEW_NT) few_product_kernel(FewArgs a) {
       e = __builtin_amdgcn_readfirstlane(q.plan.expert[slot]);
       off = __builtin_amdgcn_readfirstlane(q.plan.off[slot]);
       n = __builtin_amdgcn_readfirstlane(q.plan.n[slot]);
-      const E* wr = reinterpret_cast<const E*>(a.W) + ((int64_t)e * a.R + r0 + r16) * a.K + g * VEC;
+      const E* wt = reinterpret_cast<const E*>(a.W) + ((int64_t)e * a.R + r0) * a.K;
       auto row = [&](int i) {              // the operand row of the expert's i-th row (the last one past its end)
         const int r = off + min(i, n - 1);
         return in + (int64_t)(UP ? q.plan.rowpair[r] / a.gate.k : r) * a.K + g * VEC;
       };
       if (MAXQ == 1 || n <= 16) {
         const E* xr[1] = {row(r16)};
-        few_tile<E, 1, 8>(wr, xr, c0, c1, reinterpret_cast<f32x4_t(&)[1]>(acc));
+        few_tile<E, 1, 8>(wt, a.K, xr, c0, c1, q.turn[wv], reinterpret_cast<f32x4_t(&)[1]>(acc));
       } else if constexpr (MAXQ == 4) {
         if (n <= 32) {
           const E* xr[2] = {row(r16), row(16 + r16)};
-          few_tile<E, 2, 4>(wr, xr, c0, c1, reinterpret_cast<f32x4_t(&)[2]>(acc));
+          few_tile<E, 2, 4>(wt, a.K, xr, c0, c1, q.turn[wv], reinterpret_cast<f32x4_t(&)[2]>(acc));
         } else {
           const E* xr[4] = {row(r16), row(16 + r16), row(32 + r16), row(48 + r16)};
-          few_tile<E, 4, 4>(wr, xr, c0, c1, acc);
+          few_tile<E, 4, 4>(wt, a.K, xr, c0, c1, q.turn[wv], acc);
         }
       }
     }
@@ -410,7 +477,7 @@ template <typename E, bool UP, bool INLINE, bool ALIVE>
 static void few_product(const Shape& s, const FewArgs& a, hipStream_t st) {
   const int ks = few_split(s, a.R, a.K);
   const int64_t tiles = std::min(s.P, s.N) * (a.R / 16), tpb = FEW_NW / ks;
-  const dim3 grid((unsigned)std::min<int64_t>((tiles + tpb - 1) / tpb, 512));
+  const dim3 grid((unsigned)std::min<int64_t>((tiles + tpb - 1) / tpb, 256));
   auto go = [&](auto KSc) {
     constexpr int KS = decltype(KSc)::value;
     if (ks != KS) return;
@@ -431,10 +498,14 @@ static void layer_few_fwd(const Shape& s, const GateArgs& g, const void* W1, con
   double* part = reinterpret_cast<double*>(ws + L.part);
   FewPlan* plan = reinterpret_cast<FewPlan*>(ws + L.plan);
   const bool alive_first = (s.flags & DMOE_FLAG_ALIVE_TOPK) != 0;
-  const int CTN = (int)((s.dM + 15) / 16), units = (int)((s.T + 15) / 16) * CTN * L.S;
-  DMOE_LAUNCH_NAMED("few_scores_kernel", few_scores_kernel<E>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, g, part,
-                    CTN, L.S, units);
   const bool inl = s.T <= FEW_NW;
+  if (inl && s.T * s.dM * s.D <= FEW_INLINE) {
+    part = nullptr;
+  } else {
+    const int CTN = (int)((s.dM + 15) / 16), units = (int)((s.T + 15) / 16) * CTN * L.S;
+    DMOE_LAUNCH_NAMED("few_scores_kernel", few_scores_kernel<E>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, g,
+                      part, CTN, L.S, units);
+  }
   if (!inl) {
     auto kern = alive_first ? few_select_kernel<E, true> : few_select_kernel<E, false>;
     DMOE_LAUNCH_NAMED("few_select_kernel", kern, dim3((unsigned)((s.T + FEW_NW - 1) / FEW_NW)), dim3(FEW_NT), 0, st, g, part,
