@@ -394,6 +394,39 @@ int dmoe_layer_few_fwd(const dmoe_dims* dims, const void* x, const void* Wg, con
                        void* stream);
 size_t dmoe_layer_few_workspace_bytes(const dmoe_dims* dims);
 
+/* ------------------------------------------------------------------------------
+ * Orthogonalised updates of expert and gate matrices, beside the gradient descent of
+ * dmoe_expert_ffn_bwd_sgd.  A batch of B matrices [B, m, n], contiguous: a stack of expert
+ * weights ([N, H, D], [N, D, H]) or the d gate layers ([d, M, D]), and their gradients.  m and n
+ * are any sizes from 1 to 32768, B at most 16384, steps 1 to 64 (5 is usual); beyond:
+ * DMOE_EUNSUPPORTED.
+ * ------------------------------------------------------------------------------ */
+typedef struct {
+  int64_t B, m, n;   /* matrices, rows, columns */
+  int32_t dtype;     /* DMOE_F32 or DMOE_BF16, of G, O and W */
+  int32_t steps;     /* Newton-Schulz steps */
+} dmoe_mats;
+
+/* O_e = NS(G_e) for every matrix e, the Newton-Schulz form of U V^T for G = U S V^T: with
+ * X [min(m, n), max(m, n)] the matrix or its transpose,
+ *   X = G / (|G|_F + 1e-7);  steps times  A = X X^T,  X = (a I + b A + c A A) X,
+ * (a, b, c) = (3.4445, -4.7750, 2.0315).  Singular values from about 0.3% of the norm up end in
+ * [0.7, 1.21] after five steps; a zero matrix gives zeros.  Products carry about 22 bits or more, whatever the type.
+ * counts [B] int32 or NULL: a matrix with counts[e] = 0 (an expert without rows, whose gradient
+ * dmoe_expert_ffn_bwd does not write) is not read, and its O left as it is.  O may be G.
+ * ws: dmoe_orthogonalize_workspace_bytes(mats) bytes (0 for invalid mats), also for
+ * dmoe_muon_step. */
+int dmoe_orthogonalize(const dmoe_mats* mats, const void* G, const int32_t* counts, void* O, void* ws,
+                       void* stream);
+
+/* One update of the matrices W with momentum:
+ *   mom = mu mom + G;  U = G + mu mom (nesterov != 0) or mom;  W = (1 - lr decay) W - lr NS(U),
+ * mom [B, m, n] fp32, W and G in the matrices' type; W is rounded once.  Matrices with counts[e] = 0
+ * keep W and mom.  G, mom and W must not overlap; lr, mu and decay must not be NaN. */
+int dmoe_muon_step(const dmoe_mats* mats, const void* G, const int32_t* counts, float* mom, void* W,
+                   float lr, float mu, float decay, int nesterov, void* ws, void* stream);
+size_t dmoe_orthogonalize_workspace_bytes(const dmoe_mats* mats);
+
 #ifdef __cplusplus
 }
 #endif

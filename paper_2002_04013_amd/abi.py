@@ -27,6 +27,7 @@ EXPORTS = (
     "dmoe_trace_begin", "dmoe_trace_end", "dmoe_expert_ffn_fwd_noalloc", "dmoe_ffn_workspace_bytes",
     "dmoe_layer_norm_fwd", "dmoe_layer_norm_bwd", "dmoe_layer_norm_workspace_bytes",
     "dmoe_layer_few_fwd", "dmoe_layer_few_workspace_bytes",
+    "dmoe_orthogonalize", "dmoe_muon_step", "dmoe_orthogonalize_workspace_bytes",
 )
 
 FEW_TOKENS = 64      # most tokens of dmoe_layer_few_fwd
@@ -46,6 +47,11 @@ class Dims(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
+class Mats(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("steps", ctypes.c_int32)]
+
+
 class FFBlockParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in FFBLOCK_PARAMS]
 
@@ -60,6 +66,10 @@ def make_dims(T, D, H, d, M, k, dtype="bf16", act="gelu", flags=0):
                 DMOE_GELU if act == "gelu" else DMOE_RELU, int(flags))
 
 
+def make_mats(B, m, n, dtype="bf16", steps=5):
+    return Mats(int(B), int(m), int(n), DMOE_BF16 if dtype == "bf16" else DMOE_F32, int(steps))
+
+
 _lib = None
 _P = ctypes.c_void_p
 
@@ -72,7 +82,7 @@ def load(path=LIB_PATH):
     if not os.path.exists(path):
         raise DmoeError(f"{path} is missing: build it with `python -m paper_2002_04013_amd.build`")
     lib = ctypes.CDLL(path)
-    pd = ctypes.POINTER(Dims)
+    pd, pm = ctypes.POINTER(Dims), ctypes.POINTER(Mats)
     sig = {
         "dmoe_workspace_bytes": (ctypes.c_size_t, [pd]),
         "dmoe_ffn_workspace_bytes": (ctypes.c_size_t, [pd]),
@@ -103,6 +113,9 @@ def load(path=LIB_PATH):
         "dmoe_layer_norm_workspace_bytes": (ctypes.c_size_t, [pd]),
         "dmoe_layer_few_fwd": (ctypes.c_int, [pd] + [_P] * 14),
         "dmoe_layer_few_workspace_bytes": (ctypes.c_size_t, [pd]),
+        "dmoe_orthogonalize": (ctypes.c_int, [pm] + [_P] * 5),
+        "dmoe_muon_step": (ctypes.c_int, [pm] + [_P] * 4 + [ctypes.c_float] * 3 + [ctypes.c_int] + [_P] * 2),
+        "dmoe_orthogonalize_workspace_bytes": (ctypes.c_size_t, [pm]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -284,6 +297,21 @@ def dmoe_layer_few_fwd(dims, x, Wg, bg, alive, W1, b1, W2, b2, res, idx, w, y, w
     _check(load().dmoe_layer_few_fwd(ctypes.byref(dims), _ptr(x), _ptr(Wg), _ptr(bg), _ptr(alive), _ptr(W1), _ptr(b1),
                                      _ptr(W2), _ptr(b2), _ptr(res), _ptr(idx), _ptr(w), _ptr(y), _ptr(ws),
                                      _stream(stream)), "dmoe_layer_few_fwd")
+
+
+def orthogonalize_workspace_bytes(mats):
+    return int(load().dmoe_orthogonalize_workspace_bytes(ctypes.byref(mats)))
+
+
+def dmoe_orthogonalize(mats, G, counts, O, ws, stream=None):
+    _check(load().dmoe_orthogonalize(ctypes.byref(mats), _ptr(G), _ptr(counts), _ptr(O), _ptr(ws), _stream(stream)),
+           "dmoe_orthogonalize")
+
+
+def dmoe_muon_step(mats, G, counts, mom, W, lr, mu, decay, nesterov, ws, stream=None):
+    _check(load().dmoe_muon_step(ctypes.byref(mats), _ptr(G), _ptr(counts), _ptr(mom), _ptr(W), ctypes.c_float(lr),
+                                 ctypes.c_float(mu), ctypes.c_float(decay), int(bool(nesterov)), _ptr(ws),
+                                 _stream(stream)), "dmoe_muon_step")
 
 
 class Trace:

@@ -1,0 +1,886 @@
+// Orthogonalised updates: Newton-Schulz steps on batches of matrices, alone and as the update of
+// a momentum step.  With r = min(m, n), c = max(m, n) and X the r x c form of a matrix U,
+//   X <- U / (|U|_F + eps);  steps times  A = X X^T,  X <- (a I + b A + c A A) X,
+// singular value by singular value s <- a s + b s^3 + c s^5, which takes (0, 1] into about [0.7, 1.2].
+//
+// The steps multiply small singular values by up to a^5 = 485 against the large ones, so what
+// rounding leaves in X of the directions that U does not have grows with them: bf16 operands
+// (2^-9 of an entry) end at several per cent of the result for gradients of low rank.  Both
+// routes therefore keep about fp32's precision:
+//
+// r > 64: the products on fp16 matrix instructions with every operand as the sum of two fp16
+// values, x 2^14 = hi + lo (22 bits; every entry is at most 3.45 in magnitude: the singular
+// values stay below 1.21, A's below 1.45, and a I + b A + c A A lies between 0.6 and a), and
+// three products hi hi + hi lo + lo hi into one fp32 accumulator.  A and Q = a I + b A + c A A are
+// symmetric: tiles of the lower triangle only, stored twice.  Bound by the fp16 matrix rate:
+// 3 (r^2 c + r^3 + 2 r^2 c) multiply-adds' flops a step.
+//
+// r <= 64: everything in the r x r space in fp64.  X_k = P_k X_0 with P_k a polynomial of
+// A_0 = X_0 X_0^T, so  Q = a I + b A + c A A,  P <- Q P,  A <- Q A Q  from A_0, P_0 = I, and
+// one product P U at the end: two passes over U whatever the steps.  (In fp32 this form loses
+// the small singular values, whose squares it iterates; in fp64 it does not.)
+#include <algorithm>
+
+#include "common.hpp"
+
+namespace dmoe {
+
+typedef _Float16 f16;
+typedef f16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef f16 f16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+
+constexpr double NS_A = 3.4445, NS_B = -4.7750, NS_C = 2.0315;
+constexpr double NS_EPS = 1e-7;
+constexpr float SPLIT = 16384.f;          // operands are held as value * SPLIT = hi + lo
+constexpr int64_t ORTHO_MAX = 32768;      // largest m, n
+constexpr int64_t GRAM_R = 64;            // largest r of the fp64 route
+
+// What the update is made of.
+struct UpdateArgs {
+  const void* G;                          // [B][m][n]
+  float* mom;                             // momentum [B][m][n], or NULL: U = G
+  void* out;                              // O, or the parameters (mom not NULL)
+  const int32_t* counts;                  // [B] or NULL; a matrix with 0 is left alone
+  int m, n, nesterov;
+  float mu, lr, keep;                     // keep = 1 - lr decay
+};
+
+__device__ __forceinline__ bool on(const UpdateArgs& a, int e) { return !a.counts || a.counts[e] > 0; }
+
+// U at N places (those with ok): FIRST advances the momentum there, later passes read it.
+// All loads come before the stores, so that they are in flight together.
+template <typename E, bool FIRST, int N>
+__device__ __forceinline__ void update_at(const UpdateArgs& a, const int64_t (&at)[N], const bool (&ok)[N], float (&u)[N]) {
+  float m[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u[i] = ok[i] ? ldf(reinterpret_cast<const E*>(a.G) + at[i]) : 0.f;
+    m[i] = a.mom && ok[i] ? a.mom[at[i]] : 0.f;
+  }
+  if (!a.mom) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (FIRST) {
+      m[i] = fmaf(a.mu, m[i], u[i]);
+      if (ok[i]) a.mom[at[i]] = m[i];
+    }
+    u[i] = a.nesterov ? fmaf(a.mu, m[i], u[i]) : m[i];
+  }
+}
+// The result at one place: O, or the step of the parameters (one rounding).
+template <typename E>
+__device__ __forceinline__ void store_at(const UpdateArgs& a, int64_t at, float o) {
+  E* p = reinterpret_cast<E*>(a.out) + at;
+  *p = cvt<E>(a.mom ? fmaf(-a.lr, o, a.keep * ldf(p)) : o);
+}
+
+// ---------------------------------------------------------------- r > 64: norm and operands
+
+constexpr int NB_MAX = 64;                // blocks to a matrix of the norm
+
+// part[e][block] = sum of U^2 over the block's share, in fp64 (squares of fp32 values overflow
+// fp32); advances the momentum.  WIDE: 16 bytes of G to a thread (m n a multiple of them), else
+// an element.
+template <typename E, bool WIDE>
+__global__ void __launch_bounds__(256) ortho_norm_kernel(UpdateArgs a, int e0, double* part) {
+  constexpr int V = WIDE ? Vec<E>::N : 4;
+  __shared__ double red[4];
+  const int e = e0 + blockIdx.y;
+  if (!on(a, e)) return;
+  const int64_t mn = (int64_t)a.m * a.n, base = e * mn;
+  const int64_t per = ((mn + gridDim.x - 1) / gridDim.x + V - 1) / V * V;
+  const int64_t i0 = blockIdx.x * per, i1 = min(mn, i0 + per);
+  double s = 0.0;
+  if constexpr (WIDE) {
+#pragma unroll 2
+    for (int64_t i = i0 + threadIdx.x * V; i < i1; i += 256 * V) {
+      float u[V];
+      Vec<E>::unpack(*reinterpret_cast<const uint4*>(reinterpret_cast<const E*>(a.G) + base + i), u);
+      if (a.mom) {
+        float4* mp = reinterpret_cast<float4*>(a.mom + base + i);
+        float4 m[V / 4];
+#pragma unroll
+        for (int k = 0; k < V / 4; ++k) m[k] = mp[k];
+#pragma unroll
+        for (int k = 0; k < V / 4; ++k) {
+          float* w = u + 4 * k;
+          m[k] = make_float4(fmaf(a.mu, m[k].x, w[0]), fmaf(a.mu, m[k].y, w[1]), fmaf(a.mu, m[k].z, w[2]),
+                             fmaf(a.mu, m[k].w, w[3]));
+          mp[k] = m[k];
+          w[0] = a.nesterov ? fmaf(a.mu, m[k].x, w[0]) : m[k].x;
+          w[1] = a.nesterov ? fmaf(a.mu, m[k].y, w[1]) : m[k].y;
+          w[2] = a.nesterov ? fmaf(a.mu, m[k].z, w[2]) : m[k].z;
+          w[3] = a.nesterov ? fmaf(a.mu, m[k].w, w[3]) : m[k].w;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < V; ++k) s = fma((double)u[k], (double)u[k], s);
+    }
+  } else {
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += 256 * V) {
+      int64_t at[V];
+      bool ok[V];
+      float u[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) { at[k] = base + i + 256 * k; ok[k] = i + 256 * k < i1; }
+      update_at<E, true>(a, at, ok, u);
+#pragma unroll
+      for (int k = 0; k < V; ++k) s = fma((double)u[k], (double)u[k], s);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[(int64_t)blockIdx.y * NB_MAX + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
+  hi = (f16)v;
+  lo = (f16)(v - (float)hi);
+}
+
+// X (hi and lo planes [Rp][Cp]) = U / (|U| + eps), padded with zeros; a block to a 64 x 64 piece,
+// turned through LDS where m > n.
+template <typename E>
+__global__ void __launch_bounds__(256)
+ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* hi, f16* lo, int Rp, int Cp, int64_t plane) {
+  __shared__ float tile[64][65];
+  __shared__ double inv;
+  const int g = blockIdx.z, e = e0 + g;
+  if (!on(a, e)) return;
+  if (threadIdx.x < 64) {
+    double s = (int)threadIdx.x < nb ? part[(int64_t)g * NB_MAX + threadIdx.x] : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
+    if (threadIdx.x == 0) inv = (double)SPLIT / (sqrt(s) + NS_EPS);
+  }
+  const bool turn = a.m > a.n;
+  const int x0 = blockIdx.x * 64, y0 = blockIdx.y * 64;            // column and row of X
+  const int i0 = turn ? x0 : y0, j0 = turn ? y0 : x0;              // of U
+  const int64_t base = (int64_t)e * a.m * a.n;
+  for (int q = threadIdx.x; q < 64 * 64; q += 8 * 256) {
+    int64_t at[8];
+    bool ok[8];
+    float u[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = i0 + ((q + 256 * k) >> 6), j = j0 + (q & 63);
+      at[k] = base + (int64_t)i * a.n + j;
+      ok[k] = i < a.m && j < a.n;
+    }
+    update_at<E, false>(a, at, ok, u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[(q + 256 * k) >> 6][q & 63] = u[k];
+  }
+  __syncthreads();
+  const double f = inv;
+  for (int q = threadIdx.x; q < 64 * 8; q += 256) {
+    const int y = q >> 3, x = (q & 7) * 8;
+    f16x8_t h, l;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      f16 vh, vl;
+      split((float)((double)(turn ? tile[x + k][y] : tile[y][x + k]) * f), vh, vl);
+      h[k] = vh; l[k] = vl;
+    }
+    const int64_t at = g * plane + (int64_t)(y0 + y) * Cp + x0 + x;
+    *reinterpret_cast<f16x8_t*>(hi + at) = h;
+    *reinterpret_cast<f16x8_t*>(lo + at) = l;
+  }
+}
+
+// ---------------------------------------------------------------- r > 64: products of split operands
+
+// 16 bytes a lane from global memory straight into the wave's 1 KiB of LDS at lds_wave_base.  Written
+// out as the instruction, so that the compiler adds no waits of its own; the loop's waits and
+// barriers order the loads.
+__device__ __forceinline__ void g2l(const f16* base, uint32_t off_bytes, char* lds_wave_base) {
+  const uint32_t m = (uint32_t)(uintptr_t)(lds_ptr_t)lds_wave_base;
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(off_bytes), "s"(base), "s"(m) : "memory", "m0");
+}
+
+constexpr int NS_BK = 32;                 // contraction of one LDS stage
+
+// Tile of R rows contiguous along the contraction, [R][32]: 16-byte chunk c of row i at position
+// c ^ ((i / 4) % 4), so that 16 rows read at one chunk fall on 16 bank groups.
+template <int R, int NW>
+struct RowTile {
+  static constexpr int BYTES = R * 64, PER_WAVE = R / 16 / NW;
+  static_assert(R % (16 * NW) == 0, "whole instructions to a wave");
+  __device__ __forceinline__ static void load(const f16* base, int ld, char* lds, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < PER_WAVE; ++i) {
+      const int q = wave + i * NW, row = q * 16 + lane / 4, c = (lane & 3) ^ ((row >> 2) & 3);
+      g2l(base, ((uint32_t)row * (uint32_t)ld + (uint32_t)(c * 8)) * 2u, lds + q * 1024);
+    }
+  }
+  // operand of rows i0 .. i0 + 31 and contraction kk .. kk + 15 (kk = 0 or 16)
+  __device__ __forceinline__ static f16x8_t frag(const char* lds, int i0, int kk, int lane) {
+    const int row = i0 + (lane & 31), c = (kk / 8 + (lane >> 5)) ^ ((row >> 2) & 3);
+    return *reinterpret_cast<const f16x8_t*>(lds + row * 64 + c * 16);
+  }
+};
+
+// Tile of R columns, [32][R], contiguous across the contraction: chunk c of row k at position
+// c ^ (4 (k % 4)); operands come from transposing reads.
+template <int R, int NW>
+struct ColTile {
+  static constexpr int BYTES = R * 64, RPI = 512 / R, PER_WAVE = R / 16 / NW;
+  __device__ __forceinline__ static void load(const f16* base, int ld, char* lds, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < PER_WAVE; ++i) {
+      const int q = wave + i * NW, k = q * RPI + lane / (R / 8), c = (lane % (R / 8)) ^ (4 * (k & 3));
+      g2l(base, ((uint32_t)k * (uint32_t)ld + (uint32_t)(c * 8)) * 2u, lds + q * 1024);
+    }
+  }
+  __device__ __forceinline__ static f16x8_t frag(const char* lds, int c0, int kk, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+    const int col = c0 + 16 * (g & 1) + 4 * (i & 3), k = kk + 8 * (g >> 1) + (i >> 2);
+    const char* at = lds + k * (2 * R) + (((col >> 3) ^ (4 * (k & 3))) << 4) + (col & 7) * 2;   // k and k + 4: same position
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(at + 4 * 2 * R));
+    const s16x8_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(f16x8_t, v);
+  }
+};
+
+// Orders the LDS operations of one wave for the compiler; the hardware keeps their order.
+__device__ __forceinline__ void wave_sync() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Every load of this wave has landed and its LDS reads are done, for the whole block.
+__device__ __forceinline__ void stage_sync() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+enum NsProduct {
+  NS_GRAM,    // A = X X^T
+  NS_POLY,    // Q = a I + b A + c A A
+  NS_APPLY,   // X' = Q X
+  NS_LAST     // the same, into O or the parameters
+};
+
+struct NsArgs {
+  const f16 *Ah, *Al, *Bh, *Bl;           // operands (hi, lo planes), matrix by matrix
+  f16 *Ch, *Cl;                           // result planes
+  float* part;                            // NS_GRAM over S slices of the contraction: their sums
+  int lda, ldb, ldc, K;                   // multiples of 32
+  int64_t sa, sb, sc;                     // strides of the matrices
+  int TI, TJ, tiles, groups, S;           // tiles of a matrix, matrices, slices
+  int e0;
+  UpdateArgs u;
+};
+
+// Tile t of a matrix: row ti, column tj.  Symmetric results: the lower triangle, row by row.
+template <int P>
+__device__ __forceinline__ void tile_at(const NsArgs& p, int t, int& ti, int& tj) {
+  if constexpr (P == NS_GRAM || P == NS_POLY) {
+    ti = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while (ti * (ti + 1) / 2 > t) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
+    tj = t - ti * (ti + 1) / 2;
+  } else {
+    ti = t % p.TI;
+    tj = t / p.TI;
+  }
+}
+
+// The value of a symmetric result from its accumulator (2^28 times the product).
+template <int P>
+__device__ __forceinline__ float ns_value(float acc, float ah, float al, int i, int j) {
+  constexpr float D = 1.f / SPLIT;
+  if constexpr (P == NS_POLY) return (float)NS_C * (acc * D) + (float)NS_B * (ah + al) + (i == j ? (float)NS_A * SPLIT : 0.f);
+  else return acc * D;
+}
+
+// One T x T tile to a block (8 waves of 128 x 64 for T = 256, 4 of 64 x 64 for 128): two LDS stages
+// of 32, the next one loaded while the current one is multiplied.
+template <typename E, int P, int T>
+__global__ void __launch_bounds__(T == 256 ? 512 : 256)
+ns_product_kernel(NsArgs p) {
+  constexpr int WM = 2, WN = T / 64, NW = WM * WN;
+  constexpr int TM = T / WM / 32, TN = 2;
+  constexpr bool SYM = P == NS_GRAM || P == NS_POLY;
+  using TA = RowTile<T, NW>;
+  using TB = typename std::conditional<SYM, RowTile<T, NW>, ColTile<T, NW>>::type;
+  constexpr int STAGE = 2 * TA::BYTES + 2 * TB::BYTES;
+  extern __shared__ __align__(1024) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+
+  // blocks are dealt to the eight XCDs in turn: each takes a contiguous run of tiles
+  const int total = p.groups * p.tiles * p.S;
+  const int L = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+  if (L >= total) return;
+  const int s = L % p.S, t = L / p.S % p.tiles, g = L / p.S / p.tiles;
+  if (!on(p.u, p.e0 + g)) return;
+  int ti, tj;
+  tile_at<P>(p, t, ti, tj);
+  const int nk_all = p.K / NS_BK, k0 = nk_all * s / p.S, nk = nk_all * (s + 1) / p.S - k0;
+  const int64_t oa = g * p.sa + (int64_t)ti * T * p.lda + k0 * NS_BK;
+  const int64_t ob = g * p.sb + (SYM ? (int64_t)tj * T * p.ldb + k0 * NS_BK : (int64_t)tj * T);
+  auto load = [&](int k) {
+    char* st = smem + (k & 1) * STAGE;
+    const int64_t a = oa + k * NS_BK, b = ob + (SYM ? (int64_t)k * NS_BK : (int64_t)k * NS_BK * p.ldb);
+    TA::load(p.Ah + a, p.lda, st, wave, lane);
+    TA::load(p.Al + a, p.lda, st + TA::BYTES, wave, lane);
+    TB::load(p.Bh + b, p.ldb, st + 2 * TA::BYTES, wave, lane);
+    TB::load(p.Bl + b, p.ldb, st + 2 * TA::BYTES + TB::BYTES, wave, lane);
+  };
+
+  // results along rows (turned: along columns): the lane's 4 consecutive results are the matrix
+  // instruction's first operand's
+  const bool turn = P == NS_LAST && p.u.m > p.u.n;
+  f32x16_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+  auto run = [&](auto TURN) {
+    load(0);
+    for (int k = 0; k < nk; ++k) {
+      stage_sync();
+      if (k + 1 < nk) load(k + 1);
+      const char* st = smem + (k & 1) * STAGE;
+#pragma unroll
+      for (int kk = 0; kk < NS_BK; kk += 16) {
+        f16x8_t ah[TM], al[TM], bh[TN], bl[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const int c0 = wn * 64 + j * 32;
+          bh[j] = TB::frag(st + 2 * TA::BYTES, c0, kk, lane);
+          bl[j] = TB::frag(st + 2 * TA::BYTES + TB::BYTES, c0, kk, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const int r0 = wm * (T / WM) + i * 32;
+          ah[i] = TA::frag(st, r0, kk, lane);
+          al[i] = TA::frag(st + TA::BYTES, r0, kk, lane);
+        }
+        auto mma = [&](const f16x8_t& a, const f16x8_t& b, f32x16_t c) {
+          if constexpr (TURN.value) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+          else return __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, c, 0, 0, 0);
+        };
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = mma(ah[i], bl[j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = mma(al[i], bh[j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = mma(ah[i], bh[j], acc[i][j]);
+      }
+    }
+  };
+  if constexpr (P == NS_LAST) {
+    if (turn) run(std::true_type{});
+    else run(std::false_type{});
+  } else {
+    run(std::false_type{});
+  }
+
+  const int i0 = ti * T + wm * (T / WM), j0 = tj * T + wn * 64;      // the wave's rows and columns
+  const int lp = lane & 31, lq = (lane >> 5) * 4;                    // element v: q = 8 (v / 4) + lq + v % 4 of line p = lp
+
+  if constexpr (P == NS_GRAM) {
+    if (p.S > 1) {
+      // the slices' sums are added, and the results stored, by ns_finish_kernel
+      float* o = p.part + ((int64_t)L * NW + wave) * TM * TN * 1024 + lane * 16;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4)
+            *reinterpret_cast<float4*>(o + (i * TN + j) * 1024 + v) =
+                make_float4(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
+      return;
+    }
+  }
+  stage_sync();                              // the ring is free: 16 KiB of it to a wave
+  char* mine = smem + wave * 16384;
+
+  if constexpr (P == NS_LAST) {
+    // 32 x 32 results at a time through LDS in fp32, then line by line
+    float* buf = reinterpret_cast<float*>(mine);
+    const int64_t base = (int64_t)(p.e0 + g) * p.u.m * p.u.n;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<float4*>(buf + lp * 36 + 2 * v + lq) =
+              make_float4(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
+        wave_sync();
+        const int ib = i0 + i * 32, jb = j0 + j * 32;
+        const int row0 = turn ? jb : ib, col = (turn ? ib : jb) + lp;
+#pragma unroll 4
+        for (int q = lane >> 5; q < 32; q += 2) {
+          const int row = row0 + q;
+          const float o = buf[q * 36 + lp] * (1.f / (SPLIT * SPLIT));
+          if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + (int64_t)row * p.u.n + col, o);
+        }
+        wave_sync();
+      }
+    return;
+  }
+
+  // the results split again: 32 rows x 64 columns of each plane at a time through LDS, 128-byte rows
+  f16* Ch = p.Ch + g * p.sc;
+  f16* Cl = p.Cl + g * p.sc;
+  const f16* Xh = p.Ah + g * p.sa;
+  const f16* Xl = p.Al + g * p.sa;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int row = i0 + i * 32 + lp;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4) {
+        const int col = j0 + j * 32 + 2 * v + lq;
+        f16x4_t h4 = {}, l4 = {}, h, l;
+        if constexpr (P == NS_POLY) {
+          h4 = *reinterpret_cast<const f16x4_t*>(Xh + (int64_t)row * p.lda + col);
+          l4 = *reinterpret_cast<const f16x4_t*>(Xl + (int64_t)row * p.lda + col);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float val = ns_value<P>(acc[i][j][v + q], (float)h4[q], (float)l4[q], row, col + q);
+          acc[i][j][v + q] = val;
+          f16 vh, vl;
+          split(val, vh, vl);
+          h[q] = vh; l[q] = vl;
+        }
+        // chunk of 8 columns 4 j + v / 4 of row lp, at position ^ row % 8
+        char* at = mine + lp * 128 + (((4 * j + v / 4) ^ (lp & 7)) << 4) + lq * 2;
+        *reinterpret_cast<f16x4_t*>(at) = h;
+        *reinterpret_cast<f16x4_t*>(at + 4096) = l;
+      }
+    wave_sync();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = q * 8 + (lane >> 3), c = lane & 7;
+      const char* at = mine + r * 128 + ((c ^ (r & 7)) << 4);
+      const int64_t o = (int64_t)(i0 + i * 32 + r) * p.ldc + j0 + c * 8;
+      *reinterpret_cast<f16x8_t*>(Ch + o) = *reinterpret_cast<const f16x8_t*>(at);
+      *reinterpret_cast<f16x8_t*>(Cl + o) = *reinterpret_cast<const f16x8_t*>(at + 4096);
+    }
+    wave_sync();
+  }
+  if constexpr (SYM) {
+    if (ti == tj) return;
+    // and turned: 64 columns become rows of 64
+#pragma unroll
+    for (int i = 0; i < TM; i += 2) {
+#pragma unroll
+      for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            f16 vh, vl;
+            split(acc[i + ii][j][v], vh, vl);
+            const int y = j * 32 + 8 * (v / 4) + lq + v % 4, x = ii * 32 + lp;      // row and column of the 64 x 64
+            char* at = mine + y * 128 + (((x >> 3) ^ (y & 7)) << 4) + (x & 7) * 2;
+            *reinterpret_cast<f16*>(at) = vh;
+            *reinterpret_cast<f16*>(at + 8192) = vl;
+          }
+      wave_sync();
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int r = q * 8 + (lane >> 3), c = lane & 7;
+        const char* at = mine + r * 128 + ((c ^ (r & 7)) << 4);
+        const int64_t o = (int64_t)(j0 + r) * p.ldc + i0 + i * 32 + c * 8;
+        *reinterpret_cast<f16x8_t*>(Ch + o) = *reinterpret_cast<const f16x8_t*>(at);
+        *reinterpret_cast<f16x8_t*>(Cl + o) = *reinterpret_cast<const f16x8_t*>(at + 8192);
+      }
+      wave_sync();
+    }
+  }
+}
+
+// A of a product whose contraction was split over S blocks: a wave to a 32 x 32 piece adds the slices in
+// order and stores it, and its mirror image.
+template <int T>
+__global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
+  constexpr int WN = T / 64, NW = 2 * WN, TM = T / 64, TN = 2, PIECES = NW * TM * TN;
+  const int piece = blockIdx.x % PIECES, gt = blockIdx.x / PIECES, g = gt / p.tiles, t = gt % p.tiles;
+  if (!on(p.u, p.e0 + g)) return;
+  int ti, tj;
+  tile_at<NS_GRAM>(p, t, ti, tj);
+  const int lane = threadIdx.x, wave = piece / (TM * TN), i = piece / TN % TM, j = piece % TN;
+  f32x4_t acc[4] = {};
+#pragma unroll 4
+  for (int s = 0; s < p.S; ++s) {
+    const float* o = p.part + (((int64_t)gt * p.S + s) * PIECES + piece) * 1024 + lane * 16;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) acc[v] += *reinterpret_cast<const f32x4_t*>(o + 4 * v);
+  }
+  const int i0 = ti * T + wave / WN * (T / 2) + i * 32, j0 = tj * T + wave % WN * 64 + j * 32;
+  f16* Ch = p.Ch + g * p.sc;
+  f16* Cl = p.Cl + g * p.sc;
+  const int row = i0 + (lane & 31);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const int col = j0 + 8 * v + (lane >> 5) * 4;
+    f16x4_t h, l;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      f16 vh, vl;
+      split(acc[v][q] * (1.f / SPLIT), vh, vl);
+      h[q] = vh; l[q] = vl;
+      if (ti != tj) {
+        Ch[(int64_t)(col + q) * p.ldc + row] = vh;
+        Cl[(int64_t)(col + q) * p.ldc + row] = vl;
+      }
+    }
+    *reinterpret_cast<f16x4_t*>(Ch + (int64_t)row * p.ldc + col) = h;
+    *reinterpret_cast<f16x4_t*>(Cl + (int64_t)row * p.ldc + col) = l;
+  }
+}
+
+// ---------------------------------------------------------------- r <= 64: the r x r space in fp64
+
+constexpr int GR_COLS = 128;              // columns of X in LDS
+constexpr int GR_SLICES = 32;             // most partial sums of A_0
+constexpr int GR_NT = 256;
+
+// Columns c0 .. c0 + GR_COLS - 1 of X = U (not normalised), fp32 in LDS, zeros past r and c.
+template <typename E, bool FIRST>
+__device__ __forceinline__ void gram_slice(const UpdateArgs& a, int64_t base, int c0, float (*x)[GR_COLS + 4]) {
+  const bool turn = a.m > a.n;
+  const int r = turn ? a.n : a.m, c = turn ? a.m : a.n;
+  const int total = (r + 15) / 16 * 16 * GR_COLS;
+  for (int q0 = threadIdx.x; q0 < total; q0 += 8 * GR_NT) {
+    int64_t at[8];
+    int where[8];
+    bool ok[8];
+    float u[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      // along the rows of U: of X, or (turned) its columns, the rows past r after all columns
+      const int q = q0 + k * GR_NT;
+      int i = q / GR_COLS, j = q % GR_COLS;
+      if (turn && q < r * GR_COLS) { j = q / r; i = q - j * r; }
+      ok[k] = i < r && c0 + j < c;
+      at[k] = base + (turn ? (int64_t)(c0 + j) * a.n + i : (int64_t)i * a.n + c0 + j);
+      where[k] = i * (GR_COLS + 4) + j;
+    }
+    update_at<E, FIRST>(a, at, ok, u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (q0 + k * GR_NT < total) x[0][where[k]] = u[k];
+  }
+  __syncthreads();
+}
+
+// part[e][block] [R16][R16] = U U^T over the block's columns, fp64; a wave keeps up to four of
+// its 16 x 16 tiles.
+template <typename E>
+__global__ void __launch_bounds__(GR_NT) gram_kernel(UpdateArgs a, double* part) {
+  __shared__ float x[GRAM_R][GR_COLS + 4];
+  const int e = blockIdx.y;
+  if (!on(a, e)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nt = (min(a.m, a.n) + 15) / 16, R16 = nt * 16;
+  const int g = lane >> 4, c = max(a.m, a.n), pieces = (c + GR_COLS - 1) / GR_COLS;
+  f64x4_t acc[4] = {};
+  for (int s = blockIdx.x; s < pieces; s += gridDim.x) {
+    __syncthreads();
+    gram_slice<E, true>(a, (int64_t)e * a.m * a.n, s * GR_COLS, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = wave + 4 * i;
+      if (t >= nt * nt) continue;
+      const float* xi = x[t / nt * 16 + (lane & 15)];
+      const float* xj = x[t % nt * 16 + (lane & 15)];
+#pragma unroll 8
+      for (int k = 0; k < GR_COLS; k += 4)
+        acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)xi[k + g], (double)xj[k + g], acc[i], 0, 0, 0);
+    }
+  }
+  double* o = part + ((int64_t)e * gridDim.x + blockIdx.x) * R16 * R16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = wave + 4 * i;
+    if (t < nt * nt)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[(t / nt * 16 + 4 * v + (lane >> 4)) * R16 + t % nt * 16 + (lane & 15)] = acc[i][v];
+  }
+}
+
+// C = s1 A B + s2 D + s3 I of R x R matrices in LDS (R = 16 nt, leading dimension GRAM_R + 1).
+constexpr int GL = GRAM_R + 1;
+__device__ __forceinline__ void mat_mul(double* C, const double* A, const double* B, int nt, double s1, const double* D,
+                                        double s2, double s3) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();
+  for (int t = wave; t < nt * nt; t += GR_NT / 64) {
+    const int ti = t / nt * 16, tj = t % nt * 16;
+    f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
+    const double* ai = A + (ti + (lane & 15)) * GL + (lane >> 4);
+    const double* bj = B + (lane >> 4) * GL + tj + (lane & 15);
+    for (int k0 = 0; k0 < nt * 16; k0 += 16)
+#pragma unroll
+      for (int k = 0; k < 16; k += 4) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(ai[k0 + k], bj[(k0 + k) * GL], acc, 0, 0, 0);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int i = ti + 4 * v + (lane >> 4), j = tj + (lane & 15);
+      C[i * GL + j] = s1 * acc[v] + (D ? s2 * D[i * GL + j] : 0.0) + (i == j ? s3 : 0.0);
+    }
+  }
+}
+
+// P[e] [R16][R16]: the polynomial of all steps, times 1 / (|U| + eps).  A block to a matrix.
+__global__ void __launch_bounds__(GR_NT) gram_steps_kernel(UpdateArgs a, const double* part, int slices, int steps, double* P) {
+  extern __shared__ __align__(16) char smem[];
+  double* A = reinterpret_cast<double*>(smem);
+  double* Q = A + GRAM_R * GL;
+  double* Z = Q + GRAM_R * GL;
+  double* Pl = Z + GRAM_R * GL;
+  __shared__ double inv;
+  const int e = blockIdx.x;
+  if (!on(a, e)) return;
+  const int nt = (min(a.m, a.n) + 15) / 16, R16 = nt * 16;
+  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) {
+    const int i = q / R16, j = q % R16;
+    double s = 0.0;
+    const double* src = part + (int64_t)e * slices * R16 * R16 + q;
+#pragma unroll 8
+    for (int k = 0; k < slices; ++k) s += src[(int64_t)k * R16 * R16];
+    A[i * GL + j] = s;
+    Pl[i * GL + j] = i == j ? 1.0 : 0.0;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    double s = (int)threadIdx.x < R16 ? A[threadIdx.x * GL + threadIdx.x] : 0.0;      // |U|^2
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
+    if (threadIdx.x == 0) inv = 1.0 / (sqrt(s) + NS_EPS);
+  }
+  __syncthreads();
+  const double f = inv;
+  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) A[q / R16 * GL + q % R16] *= f * f;
+  for (int k = 0; k < steps; ++k) {
+    mat_mul(Q, A, A, nt, NS_C, A, NS_B, NS_A);
+    mat_mul(Z, Q, Pl, nt, 1.0, nullptr, 0.0, 0.0);
+    double* t = Pl; Pl = Z; Z = t;
+    if (k + 1 < steps) {
+      mat_mul(Z, Q, A, nt, 1.0, nullptr, 0.0, 0.0);
+      mat_mul(A, Z, Q, nt, 1.0, nullptr, 0.0, 0.0);
+    }
+  }
+  __syncthreads();
+  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) P[(int64_t)e * R16 * R16 + q] = Pl[q / R16 * GL + q % R16] * f;
+}
+
+// O (or the parameters) = P U, slice by slice.
+template <typename E>
+__global__ void __launch_bounds__(GR_NT) gram_apply_kernel(UpdateArgs a, const double* P) {
+  __shared__ float x[GRAM_R][GR_COLS + 4];
+  const int e = blockIdx.y;
+  if (!on(a, e)) return;
+  const int64_t base = (int64_t)e * a.m * a.n;
+  const int c0 = blockIdx.x * GR_COLS;
+  const bool turn = a.m > a.n;
+  const int r = turn ? a.n : a.m, c = turn ? a.m : a.n;
+  gram_slice<E, false>(a, base, c0, x);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nt = (r + 15) / 16, R16 = nt * 16;
+  const double* Pe = P + (int64_t)e * R16 * R16;
+  constexpr int CT = GR_COLS / 16;
+  for (int t = wave; t < nt * CT; t += GR_NT / 64) {
+    const int ti = t / CT * 16, tj = t % CT * 16;
+    f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
+    for (int k0 = 0; k0 < R16; k0 += 16)
+#pragma unroll
+      for (int k1 = 0; k1 < 16; k1 += 4) {
+        const int k = k0 + k1 + (lane >> 4);
+        const double pk = Pe[(ti + (lane & 15)) * R16 + k], xk = (double)x[k][tj + (lane & 15)];
+        acc = __builtin_amdgcn_mfma_f64_16x16x4f64(turn ? xk : pk, turn ? pk : xk, acc, 0, 0, 0);
+      }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      // 16 lanes along a row of the result
+      const int i = ti + (turn ? lane & 15 : 4 * v + (lane >> 4)), j = c0 + tj + (turn ? 4 * v + (lane >> 4) : lane & 15);
+      if (i < r && j < c) store_at<E>(a, base + (turn ? (int64_t)j * a.n + i : (int64_t)i * a.n + j), (float)acc[v]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+struct OrthoPlan {
+  bool gram;                              // the fp64 route
+  int64_t r, c, Rp, Cp;
+  int group;                              // matrices at a time
+  int slices, nb, S;                      // fp64 route's slices; blocks of the norm; slices of A's contraction
+  size_t part, P, xh[2], xl[2], ah, al, qh, ql, sums, total;
+};
+
+static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
+  if (!q) return DMOE_EINVAL;
+  if (q->B < 0 || q->m < 1 || q->n < 1 || q->steps < 1) return DMOE_EINVAL;
+  if (q->dtype != DMOE_F32 && q->dtype != DMOE_BF16) return DMOE_EINVAL;
+  if (q->m > ORTHO_MAX || q->n > ORTHO_MAX || q->B > 16384 || q->steps > 64) return DMOE_EUNSUPPORTED;
+  auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+  *o = OrthoPlan{};
+  o->r = std::min(q->m, q->n);
+  o->c = std::max(q->m, q->n);
+  o->gram = o->r <= GRAM_R;
+  size_t off = 0;
+  if (o->gram) {
+    const int64_t R16 = (o->r + 15) / 16 * 16;
+    o->slices = (int)std::min<int64_t>(GR_SLICES, (o->c + GR_COLS - 1) / GR_COLS);
+    o->part = off; off += up((size_t)q->B * o->slices * R16 * R16 * sizeof(double));
+    o->P = off; off += up((size_t)q->B * R16 * R16 * sizeof(double));
+    o->total = std::max<size_t>(off, 256);
+    return DMOE_OK;
+  }
+  // padded to whole 256 x 256 tiles where that is at most an eighth more, else to 128 x 128 ones
+  auto pad = [](int64_t v) { return v >= 1024 ? (v + 255) / 256 * 256 : (v + 127) / 128 * 128; };
+  o->Rp = pad(o->r);
+  o->Cp = pad(o->c);
+  // matrices at a time: enough 128 x 128 tiles for 16 rounds of the compute units, two to each
+  const int64_t tiles = o->Rp / 128 * (o->Cp / 128);
+  o->group = (int)std::max<int64_t>(1, std::min<int64_t>(q->B, (8192 + tiles - 1) / tiles));
+  o->nb = (int)std::max<int64_t>(1, std::min<int64_t>(NB_MAX, q->m * q->n / 4096));
+  // few tiles: A's contraction in slices of at least 512
+  const int64_t tri = o->Rp / 128 * (o->Rp / 128 + 1) / 2 * std::min<int64_t>(o->group, q->B ? q->B : 1);
+  o->S = (int)std::max<int64_t>(1, std::min<int64_t>({32, o->Cp / 512, 512 / tri}));
+  const size_t g = (size_t)o->group;
+  o->part = off; off += up(g * NB_MAX * sizeof(double));
+  for (size_t* p : {&o->xh[0], &o->xl[0], &o->xh[1], &o->xl[1]}) { *p = off; off += up(g * o->Rp * o->Cp * 2); }
+  for (size_t* p : {&o->ah, &o->al, &o->qh, &o->ql}) { *p = off; off += up(g * o->Rp * o->Rp * 2); }
+  if (o->S > 1) { o->sums = off; off += up((size_t)tri * o->S * 128 * 128 * sizeof(float)); }
+  o->total = off;
+  return DMOE_OK;
+}
+
+template <typename E, int P>
+static void ns_product(NsArgs p, int64_t rows, int64_t cols, int S, hipStream_t st) {
+  // 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one
+  auto tiles = [&](int64_t T) {
+    const int64_t a = rows / T, b = cols / T;
+    return (P == NS_GRAM || P == NS_POLY) ? a * (a + 1) / 2 : a * b;
+  };
+  const bool whole = rows % 256 == 0 && cols % 256 == 0;
+  const int64_t n256 = p.groups * tiles(256), n128 = p.groups * tiles(128);
+  const double t256 = (double)((n256 + 255) / 256), t128 = 0.6 * (double)((n128 + 511) / 512);
+  auto go = [&](auto Tc) {
+    constexpr int T = decltype(Tc)::value;
+    p.TI = (int)(rows / T); p.TJ = (int)(cols / T); p.tiles = (int)tiles(T); p.S = S;
+    const int64_t total = (int64_t)p.groups * p.tiles * S;
+    constexpr int lds = 2 * 4 * T * 64;
+    auto kern = ns_product_kernel<E, P, T>;
+    if (lds > 65536) {
+      (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      (void)hipGetLastError();
+    }
+    const char* name = P == NS_GRAM ? "ns_product_kernel (X X^T)" : P == NS_POLY ? "ns_product_kernel (Q)" : "ns_product_kernel (Q X)";
+    DMOE_LAUNCH_NAMED(name, kern, dim3((unsigned)((total + 7) / 8 * 8)), dim3(T == 256 ? 512 : 256), lds, st, p);
+    if constexpr (P == NS_GRAM && T == 128)
+      if (S > 1)
+        DMOE_LAUNCH_NAMED("ns_finish_kernel", ns_finish_kernel<T>, dim3((unsigned)(p.groups * p.tiles * 16)), dim3(64), 0, st, p);
+  };
+  if (whole && S == 1 && t256 <= t128) go(std::integral_constant<int, 256>{});
+  else go(std::integral_constant<int, 128>{});
+}
+
+template <typename E>
+static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, unsigned char* ws, hipStream_t st) {
+  if (o.gram) {
+    double* part = reinterpret_cast<double*>(ws + o.part);
+    double* P = reinterpret_cast<double*>(ws + o.P);
+    const dim3 grid((unsigned)((o.c + GR_COLS - 1) / GR_COLS), (unsigned)q.B);
+    DMOE_LAUNCH_NAMED("gram_kernel", gram_kernel<E>, dim3((unsigned)o.slices, (unsigned)q.B), dim3(GR_NT), 0, st, u, part);
+    constexpr int lds = 4 * GRAM_R * GL * (int)sizeof(double);
+    (void)hipFuncSetAttribute((const void*)gram_steps_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    (void)hipGetLastError();
+    DMOE_LAUNCH(gram_steps_kernel, dim3((unsigned)q.B), dim3(GR_NT), lds, st, u, part, o.slices, q.steps, P);
+    DMOE_LAUNCH_NAMED("gram_apply_kernel", gram_apply_kernel<E>, grid, dim3(GR_NT), 0, st, u, P);
+    return;
+  }
+  auto f = [&](size_t off) { return reinterpret_cast<f16*>(ws + off); };
+  double* part = reinterpret_cast<double*>(ws + o.part);
+  const int Rp = (int)o.Rp, Cp = (int)o.Cp;
+  const int64_t sx = o.Rp * o.Cp, sr = o.Rp * o.Rp;
+  for (int64_t e0 = 0; e0 < q.B; e0 += o.group) {
+    const int g = (int)std::min<int64_t>(o.group, q.B - e0);
+    const bool wide = q.m * q.n % Vec<E>::N == 0;
+    auto norm = wide ? ortho_norm_kernel<E, true> : ortho_norm_kernel<E, false>;
+    DMOE_LAUNCH_NAMED("ortho_norm_kernel", norm, dim3(o.nb, g), dim3(256), 0, st, u, (int)e0, part);
+    DMOE_LAUNCH_NAMED("ortho_split_kernel", ortho_split_kernel<E>, dim3(Cp / 64, Rp / 64, g), dim3(256), 0, st, u, (int)e0, part,
+                      o.nb, f(o.xh[0]), f(o.xl[0]), Rp, Cp, sx);
+    for (int k = 0; k < q.steps; ++k) {
+      const int x = k & 1;
+      NsArgs p{};
+      p.groups = g; p.e0 = (int)e0; p.u = u;
+      p.part = o.S > 1 ? reinterpret_cast<float*>(ws + o.sums) : nullptr;
+      p.Ah = p.Bh = f(o.xh[x]); p.Al = p.Bl = f(o.xl[x]); p.lda = p.ldb = Cp; p.sa = p.sb = sx; p.K = Cp;
+      p.Ch = f(o.ah); p.Cl = f(o.al); p.ldc = Rp; p.sc = sr;
+      ns_product<E, NS_GRAM>(p, o.Rp, o.Rp, o.S, st);
+      p.Ah = p.Bh = f(o.ah); p.Al = p.Bl = f(o.al); p.lda = p.ldb = Rp; p.sa = p.sb = sr; p.K = Rp;
+      p.Ch = f(o.qh); p.Cl = f(o.ql);
+      ns_product<E, NS_POLY>(p, o.Rp, o.Rp, 1, st);
+      p.Ah = f(o.qh); p.Al = f(o.ql);
+      p.Bh = f(o.xh[x]); p.Bl = f(o.xl[x]); p.ldb = Cp; p.sb = sx;
+      p.Ch = f(o.xh[x ^ 1]); p.Cl = f(o.xl[x ^ 1]); p.ldc = Cp; p.sc = sx;
+      if (k + 1 < q.steps) ns_product<E, NS_APPLY>(p, o.Rp, o.Cp, 1, st);
+      else ns_product<E, NS_LAST>(p, o.Rp, o.Cp, 1, st);
+    }
+  }
+}
+
+}  // namespace dmoe
+
+using namespace dmoe;
+
+extern "C" size_t dmoe_orthogonalize_workspace_bytes(const dmoe_mats* mats) {
+  OrthoPlan o;
+  return check_mats(mats, &o) == DMOE_OK ? o.total : 0;
+}
+
+extern "C" int dmoe_orthogonalize(const dmoe_mats* mats, const void* G, const int32_t* counts, void* O, void* ws,
+                                  void* stream) {
+  OrthoPlan o;
+  int rc = check_mats(mats, &o);
+  if (rc) return rc;
+  if (mats->B == 0) return DMOE_OK;
+  if (!G || !O || !ws) return DMOE_EINVAL;
+  if (!aligned16(G) || !aligned16(O) || !aligned16(ws)) return DMOE_EUNSUPPORTED;
+  UpdateArgs u{G, nullptr, O, counts, (int)mats->m, (int)mats->n, 0, 0.f, 0.f, 0.f};
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  unsigned char* base = reinterpret_cast<unsigned char*>(ws);
+  if (mats->dtype == DMOE_BF16) orthogonalize<bf16>(*mats, o, u, base, st);
+  else orthogonalize<float>(*mats, o, u, base, st);
+  return launch_status();
+}
+
+extern "C" int dmoe_muon_step(const dmoe_mats* mats, const void* G, const int32_t* counts, float* mom, void* W, float lr,
+                              float mu, float decay, int nesterov, void* ws, void* stream) {
+  OrthoPlan o;
+  int rc = check_mats(mats, &o);
+  if (rc) return rc;
+  if (lr != lr || mu != mu || decay != decay) return DMOE_EINVAL;
+  if (mats->B == 0) return DMOE_OK;
+  if (!G || !mom || !W || !ws) return DMOE_EINVAL;
+  if (!aligned16(G) || !aligned16(mom) || !aligned16(W) || !aligned16(ws)) return DMOE_EUNSUPPORTED;
+  UpdateArgs u{G, mom, W, counts, (int)mats->m, (int)mats->n, nesterov != 0, mu, lr, 1.f - lr * decay};
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  unsigned char* base = reinterpret_cast<unsigned char*>(ws);
+  if (mats->dtype == DMOE_BF16) orthogonalize<bf16>(*mats, o, u, base, st);
+  else orthogonalize<float>(*mats, o, u, base, st);
+  return launch_status();
+}

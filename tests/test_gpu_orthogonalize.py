@@ -1,0 +1,281 @@
+"""Orthogonalised updates against the Newton-Schulz steps in 64 bits.
+
+Error bounds.  The step maps singular values by p(s) = a s + b s^3 + c s^5; on [0, 1.21], where they stay, divided
+differences of p are at most 4.25, so an error E of X becomes at most 4.25 |E|_F (Frobenius) after one step.  What a step
+adds itself (r > 64): operands held to 2^-22 of a value (two fp16 values of 11 bits; the product of the two low parts is
+left out, 2^-22 of a product) and fp32 sums of 3 K products, of errors 6 sqrt(3 K) 2^-24 with all but 1e-8 probability (sums of
+independent roundings), against products of absolute values.  r <= 64: fp64 throughout; what is left is the
+rounding of the result."""
+import math
+
+import pytest
+import torch
+
+from paper_2002_04013_amd import abi
+
+A, B, C = 3.4445, -4.7750, 2.0315
+U = 2.0 ** -24
+LIP = 4.25
+
+
+def _steps64(u, steps, bound=False):
+    """NS(u) of a batch in 64 bits, and a bound on the Frobenius error of the library's r > 64 route."""
+    turn = u.shape[1] > u.shape[2]
+    x = u / (torch.linalg.vector_norm(u, dim=(1, 2), keepdim=True) + 1e-7)
+    x = x.transpose(1, 2).contiguous() if turn else x
+    fro = lambda t: torch.linalg.vector_norm(t, dim=(1, 2))
+    t = lambda v: v.transpose(1, 2).contiguous()
+    r, c = x.shape[1:]
+    err = 2.0 ** -22 * fro(x) + 2.0 ** -39 * math.sqrt(r * c)
+    eta = lambda k: 3 * 2.0 ** -22 + 6 * math.sqrt(3 * k) * U
+    eye = torch.eye(r, dtype=u.dtype, device=u.device)
+    for _ in range(steps):
+        g = torch.matmul(x, t(x))
+        q = A * eye + B * g + C * torch.matmul(g, g)
+        new = torch.matmul(q, x)
+        if bound:
+            dg = eta(c) * fro(torch.matmul(x.abs(), t(x.abs()))) + 2.0 ** -22 * fro(g)
+            dq = abs(B) * dg + C * (2 * 1.46 * dg + eta(r) * fro(torch.matmul(g.abs(), g.abs()))) + 2.0 ** -22 * fro(q)
+            err = LIP * err + 1.21 * dq + eta(r) * fro(torch.matmul(q.abs(), x.abs())) + 2.0 ** -22 * fro(new)
+        x = new
+    return (t(x) if turn else x), err
+
+
+def _make(Bn, m, n, dtype, seed, rank=None):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(Bn, m, n, generator=g, device="cuda")
+    if rank:
+        x = torch.matmul(torch.randn(Bn, m, rank, generator=g, device="cuda"), torch.randn(Bn, rank, n, generator=g, device="cuda"))
+    return (x * 0.01).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+
+
+def _call(G, steps=5, counts=None, out=None):
+    Bn, m, n = G.shape
+    mats = abi.make_mats(Bn, m, n, "f32" if G.dtype == torch.float32 else "bf16", steps)
+    ws = torch.full((abi.orthogonalize_workspace_bytes(mats),), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(G, float("nan")) if out is None else out
+    abi.dmoe_orthogonalize(mats, G, counts, out, ws)
+    return out
+
+
+def _half(dtype):
+    return U if dtype == "f32" else torch.finfo(torch.bfloat16).eps / 2
+
+
+# (matrices, m, n, rank): every side of the borders 64 / 65, 128, 1024, odd sizes, both orientations, one entry
+SMALL = [(1, 1, 1, None), (3, 1, 7, None), (2, 9, 1, None), (2, 16, 4096, None), (5, 17, 33, None), (3, 33, 17, None), (2, 64, 64, None),
+         (2, 63, 1000, 5), (2, 1000, 64, 3), (1, 50, 5000, None), (40, 4, 200, None)]
+LARGE = [(1, 65, 65, None), (3, 65, 500, None), (3, 500, 65, None), (2, 100, 200, 10), (2, 200, 100, 10), (1, 128, 4096, None), (1, 4100, 128, None),
+         (2, 129, 129, None), (3, 300, 257, 20), (1, 300, 8192, None), (1, 513, 1030, 40), (17, 70, 90, None)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SMALL, ids=str)
+def test_short_side_to_64(shape, dtype):
+    Bn, m, n, rank = shape
+    G = _make(Bn, m, n, dtype, m * n, rank)
+    ref, _ = _steps64(G.double(), 5)
+    out = _call(G).double()
+    rms = ref.square().mean().sqrt()
+    # fp64 products, one rounding to fp32 and one to the type; 1e-9 of the size for the fp64 steps (2^-53 times
+    # the growth of what A's rounding leaves, below (4.25^2)^5 = 1.9e6, times sums of 64)
+    assert ((out - ref).abs() <= (_half(dtype) + 2 * U) * ref.abs() + 1e-7 * rms).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+def test_short_side_above_64(shape, dtype):
+    Bn, m, n, rank = shape
+    G = _make(Bn, m, n, dtype, m + n, rank)
+    ref, err = _steps64(G.double(), 5, bound=True)
+    out = _call(G)
+    off = torch.linalg.vector_norm(out.double() - ref, dim=(1, 2))
+    assert (off <= err + _half(dtype) * (torch.linalg.vector_norm(ref, dim=(1, 2)) + err)).all(), (off / err).max().item()
+    if dtype == "f32":
+        # operands of 22 bits where a plain fp32 evaluation has 24: at most four times its error, and its own again
+        x = G / (torch.linalg.vector_norm(G, dim=(1, 2), keepdim=True) + 1e-7)
+        x = x.transpose(1, 2).contiguous() if m > n else x
+        for _ in range(5):
+            g = torch.matmul(x, x.transpose(1, 2).contiguous())
+            x = A * x + torch.matmul(B * g + C * torch.matmul(g, g), x)
+        plain = torch.linalg.vector_norm((x.transpose(1, 2) if m > n else x).double() - ref, dim=(1, 2))
+        assert (off <= 5 * plain + 2 * U * torch.linalg.vector_norm(ref, dim=(1, 2))).all(), (off / plain).max().item()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(16, 1024, 1024), (15, 1021, 1279), (12, 1279, 1021), (130, 1024, 1024)], ids=str)
+def test_large_tiles_and_groups(shape):
+    """Enough work for 256 x 256 tiles, and (130 matrices) more than one group."""
+    G = _make(*shape, "f32", 5)
+    out = _call(G)
+    for i in range(0, shape[0], 13):
+        ref, err = _steps64(G[i:i + 13].double(), 5, bound=True)
+        off = torch.linalg.vector_norm(out[i:i + 13].double() - ref, dim=(1, 2))
+        assert (off <= err).all(), (off / err).max().item()
+        assert (off <= 1e-4 * torch.linalg.vector_norm(ref, dim=(1, 2))).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("steps", [1, 2, 3, 8])
+@pytest.mark.parametrize("shape", [(2, 20, 70), (2, 150, 130)], ids=str)
+def test_other_numbers_of_steps(shape, steps):
+    G = _make(*shape, "f32", steps)
+    ref, err = _steps64(G.double(), steps, bound=True)
+    off = torch.linalg.vector_norm(_call(G, steps).double() - ref, dim=(1, 2))
+    assert (off <= err + 1e-6 * torch.linalg.vector_norm(ref, dim=(1, 2))).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(5, 40, 90), (5, 90, 80)], ids=str)
+def test_zero_large_tiny_and_not_finite(shape):
+    """A zero matrix gives zeros, norms past fp32's squares are finite, a matrix of NaN or infinity spoils itself only."""
+    Bn, m, n = shape
+    G = _make(Bn, m, n, "f32", 9)
+    G[1] = 0
+    G[2] *= 1e30
+    G[3] *= 1e-20
+    G[4, 0, 0] = float("inf")
+    out = _call(G)
+    ref, err = _steps64(G[:4].double(), 5, bound=True)
+    off = torch.linalg.vector_norm(out[:4].double() - ref, dim=(1, 2))
+    assert (off <= err + 1e-6 * torch.linalg.vector_norm(ref, dim=(1, 2))).all()
+    assert not out[1].any() and torch.isnan(out[4]).any() and torch.isfinite(out[:4]).all()
+    s = torch.linalg.svdvals(out[[0, 2]].double())
+    assert s.max() < 1.22 and s.min() > 0.2          # of random matrices of these sizes
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(4, 24, 60), (4, 70, 200), (4, 200, 70)], ids=str)
+def test_left_out_matrices_and_in_place(shape):
+    """counts = 0: not read, not written.  O over G: the same result."""
+    G = _make(*shape, "bf16", 2)
+    ref = _call(G)
+    counts = torch.tensor([3, 0, 1, 0], dtype=torch.int32, device="cuda")
+    G2 = G.clone()
+    G2[1] = float("nan")
+    out = _call(G2, counts=counts, out=torch.full_like(G, 7.0))
+    assert torch.equal(out[[0, 2]], ref[[0, 2]]) and (out[[1, 3]] == 7).all()
+    c = G.clone()
+    assert torch.equal(_call(c, out=c), ref)
+
+
+def _muon64(G, mom, W, lr, mu, decay, nesterov):
+    mom = mu * mom + G
+    o, err = _steps64(G + mu * mom if nesterov else mom, 5, bound=True)
+    return (1 - lr * decay) * W - lr * o, mom, lr * err
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("shape", [(3, 16, 50), (3, 50, 16), (3, 66, 131), (3, 131, 66), (3, 192, 256), (3, 256, 192)], ids=str)
+def test_momentum_step(shape, dtype, nesterov):
+    """Two updates in a row; the second matrix of three has no rows."""
+    G = [_make(*shape, dtype, 3 + i) for i in range(2)]
+    W = _make(*shape, dtype, 6) * 3
+    mom = _make(*shape, "f32", 7)
+    counts = torch.tensor([5, 0, 1], dtype=torch.int32, device="cuda")
+    mats = abi.make_mats(*shape, dtype)
+    ws = torch.full((abi.orthogonalize_workspace_bytes(mats),), 255, dtype=torch.uint8, device="cuda")
+    lr, mu, decay = 0.25, 0.875, 0.125           # exact in fp32, as is 1 - lr decay
+    for g in G:
+        W0, m0 = W.clone(), mom.clone()
+        wr, mr, err = _muon64(g.double(), m0.double(), W0.double(), lr, mu, decay, nesterov)
+        abi.dmoe_muon_step(mats, g, counts, mom, W, lr, mu, decay, nesterov, ws)
+        assert torch.equal(W[1], W0[1]) and torch.equal(mom[1], m0[1])
+        on = [0, 2]
+        assert ((mom.double() - mr).abs() <= 2 * U * (mu * m0.double().abs() + g.double().abs()))[on].all()
+        # the update's direction is of fp32 momentum: u once more on U, which the steps carry on at most 4.25 each
+        more = lr * LIP ** 5 * 3 * U
+        fro = lambda t: torch.linalg.vector_norm(t, dim=(1, 2))
+        tol = err + more + (_half(dtype) + 4 * U) * (fro(wr) + fro(W0.double()))
+        assert (fro(W.double() - wr) <= tol)[on].all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2, 32, 300), (2, 140, 2000), (2, 2000, 140)], ids=str)
+def test_streams_and_graph_replay(shape):
+    """Two streams with a workspace each at once; a captured update replayed over a spoilt workspace: the eager results."""
+    mats = abi.make_mats(*shape, "bf16")
+    n = abi.orthogonalize_workspace_bytes(mats)
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    G = [_make(*shape, "bf16", s) for s in (1, 2)]
+    W0, m0 = _make(*shape, "bf16", 3), _make(*shape, "f32", 4)
+    ref = [_call(g) for g in G]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    out = [torch.zeros_like(g) for g in G]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for i in range(2):
+            abi.dmoe_orthogonalize(mats, G[i], None, out[i], ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, r) for o, r in zip(out, ref))
+    We, me = W0.clone(), m0.clone()
+    for _ in range(3):
+        abi.dmoe_muon_step(mats, G[0], None, me, We, 0.1, 0.9, 0.01, True, ws[0])
+    W, m = W0.clone(), m0.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        abi.dmoe_muon_step(mats, G[0], None, m, W, 0.1, 0.9, 0.01, True, ws[1])
+    W.copy_(W0)
+    m.copy_(m0)
+    for _ in range(3):
+        ws[1].fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+    assert torch.equal(W, We) and torch.equal(m, me)
+
+
+def test_formula_on_singular_values():
+    """The matrix form against the polynomial applied to the singular values."""
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(1, 7, 12, generator=g, dtype=torch.float64)
+    u, s, v = torch.linalg.svd(x, full_matrices=False)
+    s = s / (s.square().sum().sqrt() + 1e-7)
+    for _ in range(5):
+        s = A * s + B * s ** 3 + C * s ** 5
+    assert (_steps64(x, 5)[0] - u @ torch.diag_embed(s) @ v).abs().max() < 1e-12
+    assert s.max() < 1.21 and s.min() > 0.6
+    # divided differences of p on the singular values' range
+    t = torch.linspace(-1.21, 1.21, 2001, dtype=torch.float64)
+    assert (A + 3 * B * t ** 2 + 5 * C * t ** 4).abs().max() < LIP
+
+
+P = lambda n, off=0: abi.ctypes.c_void_p((n << 20) + off)
+
+
+@pytest.mark.parametrize("what,rc", [
+    ("none", 0), ("G", -1), ("O", -1), ("ws", -1), ("m = 0", -1), ("n < 0", -1), ("B < 0", -1), ("steps = 0", -1), ("dtype", -1), ("no mats", -1),
+    ("m above 32768", -2), ("B above 16384", -2), ("65 steps", -2), ("G off by 8 bytes", -2), ("ws off by 8 bytes", -2)])
+def test_refusals_on_host(what, rc):
+    a = dict(G=P(1), counts=P(2), O=P(3), ws=P(4))
+    if what in a:
+        a[what] = None
+    if "off by" in what:
+        a[what.split()[0]] = P(9, 8)
+    q = dict(B=2, m=8, n=8, dtype=0, steps=5)
+    q.update({"none": dict(B=0), "m = 0": dict(m=0), "n < 0": dict(n=-1), "B < 0": dict(B=-1), "steps = 0": dict(steps=0),
+              "dtype": dict(dtype=2), "m above 32768": dict(m=32769), "B above 16384": dict(B=16385), "65 steps": dict(steps=65)}.get(what, {}))
+    mats = abi.Mats(*q.values())
+    ref = None if what == "no mats" else abi.ctypes.byref(mats)
+    raw = abi.load()
+    assert raw.dmoe_orthogonalize(ref, *a.values(), None) == rc
+    f = abi.ctypes.c_float
+    mom = [P(1), P(2), P(5), P(3)]
+    if what in ("none", "G", "O", "ws") or "off by" in what:
+        mom = [a["G"], P(2), P(5), a["O"]]
+    assert raw.dmoe_muon_step(ref, *mom, f(0.1), f(0.9), f(0.0), 1, a["ws"], None) == rc
+    if rc and what not in a and "off by" not in what:
+        assert raw.dmoe_orthogonalize_workspace_bytes(ref) == 0
+
+
+def test_momentum_step_refuses_nan_and_missing_momentum():
+    mats = abi.make_mats(2, 8, 8, "f32")
+    raw, f, nan = abi.load(), abi.ctypes.c_float, float("nan")
+    for lr, mu, decay in ((nan, 0.9, 0.0), (0.1, nan, 0.0), (0.1, 0.9, nan)):
+        assert raw.dmoe_muon_step(abi.ctypes.byref(mats), P(1), None, P(2), P(3), f(lr), f(mu), f(decay), 0, P(4), None) == -1
+    assert raw.dmoe_muon_step(abi.ctypes.byref(mats), P(1), None, None, P(3), f(0.1), f(0.9), f(0.0), 0, P(4), None) == -1
