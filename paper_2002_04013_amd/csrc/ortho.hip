@@ -78,6 +78,18 @@ __device__ __forceinline__ void store_at(const UpdateArgs& a, int64_t at, float 
   *p = cvt<E>(a.mom ? fmaf(-a.lr, o, a.keep * ldf(p)) : o);
 }
 
+constexpr float NS_DOWN = 1.f / (SPLIT * SPLIT);      // of a product of two operands
+// The same for 16 bytes of a row, from accumulators.
+template <typename E>
+__device__ __forceinline__ void store_row(const UpdateArgs& a, int64_t at, float (&o)[Vec<E>::N]) {
+  uint4* p = reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.out) + at);
+  float w[Vec<E>::N];
+  if (a.mom) Vec<E>::unpack(*p, w);
+#pragma unroll
+  for (int i = 0; i < Vec<E>::N; ++i) o[i] = a.mom ? fmaf(-a.lr, o[i] * NS_DOWN, a.keep * w[i]) : o[i] * NS_DOWN;
+  *p = Vec<E>::pack(o);
+}
+
 // ---------------------------------------------------------------- r > 64: norm and operands
 
 constexpr int NB_MAX = 64;                // blocks to a matrix of the norm
@@ -268,13 +280,17 @@ enum NsProduct {
 struct NsArgs {
   const f16 *Ah, *Al, *Bh, *Bl;           // operands (hi, lo planes), matrix by matrix
   f16 *Ch, *Cl;                           // result planes
-  float* part;                            // NS_GRAM over S slices of the contraction: their sums
   int lda, ldb, ldc, K;                   // multiples of 32
   int64_t sa, sb, sc;                     // strides of the matrices
-  int TI, TJ, tiles, groups, S;           // tiles of a matrix, matrices, slices
-  int e0;
+  int TI, tiles, total;                   // rows of tiles, tiles of a matrix and of all
+  int full, S;                            // tiles past `full` are split into S slices of the contraction:
+  float* part;                            // their sums
+  int e0;                                 // first matrix
   UpdateArgs u;
 };
+
+// blocks are dealt to the eight XCDs in turn: each takes a contiguous run of tiles (count a multiple of 8)
+__device__ __forceinline__ int xcd_run(int b, int count) { return (b & 7) * (count >> 3) + (b >> 3); }
 
 // Tile t of a matrix: row ti, column tj.  Symmetric results: the lower triangle, row by row.
 template <int P>
@@ -313,17 +329,18 @@ ns_product_kernel(NsArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
 
-  // blocks are dealt to the eight XCDs in turn: each takes a contiguous run of tiles
-  const int total = p.groups * p.tiles * p.S;
-  const int L = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
-  if (L >= total) return;
-  const int s = L % p.S, t = L / p.S % p.tiles, g = L / p.S / p.tiles;
+  const bool sliced = (int)blockIdx.x >= p.full;
+  const int u = sliced ? xcd_run((int)blockIdx.x - p.full, (int)gridDim.x - p.full) : 0;
+  const int S = sliced ? p.S : 1, s = sliced ? u % S : 0;
+  const int L = sliced ? p.full + u / S : xcd_run((int)blockIdx.x, p.full);
+  if (L >= p.total) return;
+  const int t = L % p.tiles, g = L / p.tiles;
   if (!on(p.u, p.e0 + g)) return;
   int ti, tj;
   tile_at<P>(p, t, ti, tj);
-  const int nk_all = p.K / NS_BK, k0 = nk_all * s / p.S, nk = nk_all * (s + 1) / p.S - k0;
+  const int nk_all = p.K / NS_BK, k0 = nk_all * s / S, nk = nk_all * (s + 1) / S - k0;
   const int64_t oa = g * p.sa + (int64_t)ti * T * p.lda + k0 * NS_BK;
-  const int64_t ob = g * p.sb + (SYM ? (int64_t)tj * T * p.ldb + k0 * NS_BK : (int64_t)tj * T);
+  const int64_t ob = g * p.sb + (SYM ? (int64_t)tj * T * p.ldb + k0 * NS_BK : (int64_t)k0 * NS_BK * p.ldb + tj * T);
   auto load = [&](int k) {
     char* st = smem + (k & 1) * STAGE;
     const int64_t a = oa + k * NS_BK, b = ob + (SYM ? (int64_t)k * NS_BK : (int64_t)k * NS_BK * p.ldb);
@@ -394,20 +411,18 @@ ns_product_kernel(NsArgs p) {
   const int i0 = ti * T + wm * (T / WM), j0 = tj * T + wn * 64;      // the wave's rows and columns
   const int lp = lane & 31, lq = (lane >> 5) * 4;                    // element v: q = 8 (v / 4) + lq + v % 4 of line p = lp
 
-  if constexpr (P == NS_GRAM) {
-    if (p.S > 1) {
-      // the slices' sums are added, and the results stored, by ns_finish_kernel
-      float* o = p.part + ((int64_t)L * NW + wave) * TM * TN * 1024 + lane * 16;
+  if (sliced) {
+    // the slices' sums are added, and the results stored, by ns_finish_kernel
+    float* o = p.part + ((int64_t)u * NW + wave) * TM * TN * 1024 + lane * 16;
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+      for (int j = 0; j < TN; ++j)
 #pragma unroll
-          for (int v = 0; v < 16; v += 4)
-            *reinterpret_cast<float4*>(o + (i * TN + j) * 1024 + v) =
-                make_float4(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
-      return;
-    }
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<float4*>(o + (i * TN + j) * 1024 + v) =
+              make_float4(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
+    return;
   }
   stage_sync();                              // the ring is free: 16 KiB of it to a wave
   char* mine = smem + wave * 16384;
@@ -426,12 +441,23 @@ ns_product_kernel(NsArgs p) {
               make_float4(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
         wave_sync();
         const int ib = i0 + i * 32, jb = j0 + j * 32;
-        const int row0 = turn ? jb : ib, col = (turn ? ib : jb) + lp;
+        const int row0 = turn ? jb : ib, col0 = turn ? ib : jb;
+        constexpr int V = Vec<E>::N, LPR = 32 / V;                   // lanes to a row of 32
+        if (p.u.n % V == 0) {
+#pragma unroll
+          for (int q = 0; q < 32; q += 64 / LPR) {
+            const int r = q + lane / LPR, c = lane % LPR * V;
+            float o[V];
+#pragma unroll
+            for (int x = 0; x < V; x += 4) *reinterpret_cast<float4*>(o + x) = *reinterpret_cast<const float4*>(buf + r * 36 + c + x);
+            if (row0 + r < p.u.m && col0 + c < p.u.n) store_row<E>(p.u, base + (int64_t)(row0 + r) * p.u.n + col0 + c, o);
+          }
+        } else {
 #pragma unroll 4
-        for (int q = lane >> 5; q < 32; q += 2) {
-          const int row = row0 + q;
-          const float o = buf[q * 36 + lp] * (1.f / (SPLIT * SPLIT));
-          if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + (int64_t)row * p.u.n + col, o);
+          for (int q = lane >> 5; q < 32; q += 2) {
+            const int row = row0 + q, col = col0 + lp;
+            if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + (int64_t)row * p.u.n + col, buf[q * 36 + lp] * NS_DOWN);
+          }
         }
         wave_sync();
       }
@@ -512,43 +538,61 @@ ns_product_kernel(NsArgs p) {
   }
 }
 
-// A of a product whose contraction was split over S blocks: a wave to a 32 x 32 piece adds the slices in
-// order and stores it, and its mirror image.
-template <int T>
+// The tiles whose contraction was split: a wave to a 32 x 32 piece adds the slices in order and
+// stores it (and a symmetric result's mirror image).
+template <typename E, int P, int T>
 __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
-  constexpr int WN = T / 64, NW = 2 * WN, TM = T / 64, TN = 2, PIECES = NW * TM * TN;
-  const int piece = blockIdx.x % PIECES, gt = blockIdx.x / PIECES, g = gt / p.tiles, t = gt % p.tiles;
+  constexpr int WN = T / 64, TM = T / 64, TN = 2, PIECES = 2 * WN * TM * TN;
+  const int piece = blockIdx.x % PIECES, u = blockIdx.x / PIECES, L = p.full + u, g = L / p.tiles, t = L % p.tiles;
   if (!on(p.u, p.e0 + g)) return;
   int ti, tj;
-  tile_at<NS_GRAM>(p, t, ti, tj);
+  tile_at<P>(p, t, ti, tj);
   const int lane = threadIdx.x, wave = piece / (TM * TN), i = piece / TN % TM, j = piece % TN;
   f32x4_t acc[4] = {};
 #pragma unroll 4
   for (int s = 0; s < p.S; ++s) {
-    const float* o = p.part + (((int64_t)gt * p.S + s) * PIECES + piece) * 1024 + lane * 16;
+    const float* o = p.part + (((int64_t)u * p.S + s) * PIECES + piece) * 1024 + lane * 16;
 #pragma unroll
     for (int v = 0; v < 4; ++v) acc[v] += *reinterpret_cast<const f32x4_t*>(o + 4 * v);
   }
   const int i0 = ti * T + wave / WN * (T / 2) + i * 32, j0 = tj * T + wave % WN * 64 + j * 32;
-  f16* Ch = p.Ch + g * p.sc;
-  f16* Cl = p.Cl + g * p.sc;
-  const int row = i0 + (lane & 31);
+  const int lp = lane & 31, lq = (lane >> 5) * 4;
+  if constexpr (P == NS_LAST) {
+    const bool turn = p.u.m > p.u.n;
+    const int row = (turn ? j0 : i0) + lp, col0 = (turn ? i0 : j0) + lq;
+    const int64_t base = ((int64_t)(p.e0 + g) * p.u.m + row) * p.u.n;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const int col = j0 + 8 * v + (lane >> 5) * 4;
-    f16x4_t h, l;
+    for (int v = 0; v < 4; ++v)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      f16 vh, vl;
-      split(acc[v][q] * (1.f / SPLIT), vh, vl);
-      h[q] = vh; l[q] = vl;
-      if (ti != tj) {
-        Ch[(int64_t)(col + q) * p.ldc + row] = vh;
-        Cl[(int64_t)(col + q) * p.ldc + row] = vl;
+      for (int q = 0; q < 4; ++q) {
+        const int col = col0 + 8 * v + q;
+        if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + col, acc[v][q] * NS_DOWN);
       }
+  } else {
+    f16* Ch = p.Ch + g * p.sc;
+    f16* Cl = p.Cl + g * p.sc;
+    const int row = i0 + lp;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int col = j0 + 8 * v + lq;
+      f16x4_t h4 = {}, l4 = {}, h, l;
+      if constexpr (P == NS_POLY) {
+        h4 = *reinterpret_cast<const f16x4_t*>(p.Ah + g * p.sa + (int64_t)row * p.lda + col);
+        l4 = *reinterpret_cast<const f16x4_t*>(p.Al + g * p.sa + (int64_t)row * p.lda + col);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f16 vh, vl;
+        split(ns_value<P>(acc[v][q], (float)h4[q], (float)l4[q], row, col + q), vh, vl);
+        h[q] = vh; l[q] = vl;
+        if ((P == NS_GRAM || P == NS_POLY) && ti != tj) {
+          Ch[(int64_t)(col + q) * p.ldc + row] = vh;
+          Cl[(int64_t)(col + q) * p.ldc + row] = vl;
+        }
+      }
+      *reinterpret_cast<f16x4_t*>(Ch + (int64_t)row * p.ldc + col) = h;
+      *reinterpret_cast<f16x4_t*>(Cl + (int64_t)row * p.ldc + col) = l;
     }
-    *reinterpret_cast<f16x4_t*>(Ch + (int64_t)row * p.ldc + col) = h;
-    *reinterpret_cast<f16x4_t*>(Cl + (int64_t)row * p.ldc + col) = l;
   }
 }
 
@@ -721,11 +765,42 @@ __global__ void __launch_bounds__(GR_NT) gram_apply_kernel(UpdateArgs a, const d
 
 // ---------------------------------------------------------------- host
 
+// How a product of `groups` matrices is cut: T x T tiles, the tiles past `full` with their contraction
+// in S slices.
+struct NsTiling { int T, S; int64_t tiles, full, total; };
+
+// 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one.  A round of them takes
+// 2.53 / 1.54 us per 32 of the contraction (measured at K = 4096 and 16384), 1.07 where the smaller
+// ones have a unit to themselves; what a last, partly filled round would take is shortened by
+// slices, at the price of a second launch and the slices' sums through memory (10 to 20 us).
+static NsTiling ns_tiling(int64_t groups, bool sym, int64_t rows, int64_t cols, int64_t K) {
+  NsTiling best{};
+  double least = 0.0;
+  const int64_t k = K / NS_BK;
+  for (int T : {256, 128}) {
+    if (rows % T || cols % T) continue;
+    const int64_t a = rows / T, b = cols / T, slots = T == 256 ? 256 : 512;
+    const int64_t tiles = sym ? a * (a + 1) / 2 : a * b, total = groups * tiles, rem = total % slots;
+    const double c = T == 256 ? 2.53 : 1.54, alone = T == 256 ? 2.53 : 1.07;
+    for (int S = 1; S <= 32 && (S == 1 || (rem && k >= 8 * S)); ++S) {
+      const int64_t blocks = rem * S, last = blocks % slots;
+      const double rounds = (double)(blocks / slots) * c + (last == 0 ? 0.0 : last <= 256 ? alone : c);
+      const double t = (double)(total / slots * k) * c + rounds * (double)((k + S - 1) / S) +
+                       (S > 1 ? 12.0 + (double)(blocks * T * T * 8) / 5e6 : 0.0);
+      if (!best.T || t < least) {
+        least = t;
+        best = NsTiling{T, S, tiles, S > 1 ? total - rem : (total + 7) / 8 * 8, total};
+      }
+    }
+  }
+  return best;
+}
+
 struct OrthoPlan {
   bool gram;                              // the fp64 route
   int64_t r, c, Rp, Cp;
   int group;                              // matrices at a time
-  int slices, nb, S;                      // fp64 route's slices; blocks of the norm; slices of A's contraction
+  int slices, nb;                         // fp64 route's slices; blocks of the norm
   size_t part, P, xh[2], xl[2], ah, al, qh, ql, sums, total;
 };
 
@@ -756,32 +831,28 @@ static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
   const int64_t tiles = o->Rp / 128 * (o->Cp / 128);
   o->group = (int)std::max<int64_t>(1, std::min<int64_t>(q->B, (8192 + tiles - 1) / tiles));
   o->nb = (int)std::max<int64_t>(1, std::min<int64_t>(NB_MAX, q->m * q->n / 4096));
-  // few tiles: A's contraction in slices of at least 512
-  const int64_t tri = o->Rp / 128 * (o->Rp / 128 + 1) / 2 * std::min<int64_t>(o->group, q->B ? q->B : 1);
-  o->S = (int)std::max<int64_t>(1, std::min<int64_t>({32, o->Cp / 512, 512 / tri}));
   const size_t g = (size_t)o->group;
   o->part = off; off += up(g * NB_MAX * sizeof(double));
   for (size_t* p : {&o->xh[0], &o->xl[0], &o->xh[1], &o->xl[1]}) { *p = off; off += up(g * o->Rp * o->Cp * 2); }
   for (size_t* p : {&o->ah, &o->al, &o->qh, &o->ql}) { *p = off; off += up(g * o->Rp * o->Rp * 2); }
-  if (o->S > 1) { o->sums = off; off += up((size_t)tri * o->S * 128 * 128 * sizeof(float)); }
+  size_t sums = 0;
+  for (int64_t k : {(int64_t)o->group, q->B % o->group})          // whole groups and the last one
+    for (const NsTiling& t : {ns_tiling(k, true, o->Rp, o->Rp, o->Cp), ns_tiling(k, true, o->Rp, o->Rp, o->Rp),
+                              ns_tiling(k, false, o->Rp, o->Cp, o->Rp)})
+      if (t.S > 1) sums = std::max(sums, (size_t)(t.total - t.full) * t.S * t.T * t.T * sizeof(float));
+  o->sums = off; off += up(sums);
   o->total = off;
   return DMOE_OK;
 }
 
+// E: the type of the result of NS_LAST
 template <typename E, int P>
-static void ns_product(NsArgs p, int64_t rows, int64_t cols, int S, hipStream_t st) {
-  // 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one
-  auto tiles = [&](int64_t T) {
-    const int64_t a = rows / T, b = cols / T;
-    return (P == NS_GRAM || P == NS_POLY) ? a * (a + 1) / 2 : a * b;
-  };
-  const bool whole = rows % 256 == 0 && cols % 256 == 0;
-  const int64_t n256 = p.groups * tiles(256), n128 = p.groups * tiles(128);
-  const double t256 = (double)((n256 + 255) / 256), t128 = 0.6 * (double)((n128 + 511) / 512);
+static void ns_product(NsArgs p, int64_t groups, int64_t rows, int64_t cols, hipStream_t st) {
+  const NsTiling q = ns_tiling(groups, P == NS_GRAM || P == NS_POLY, rows, cols, p.K);
   auto go = [&](auto Tc) {
     constexpr int T = decltype(Tc)::value;
-    p.TI = (int)(rows / T); p.TJ = (int)(cols / T); p.tiles = (int)tiles(T); p.S = S;
-    const int64_t total = (int64_t)p.groups * p.tiles * S;
+    p.TI = (int)(rows / T); p.tiles = (int)q.tiles; p.total = (int)q.total; p.full = (int)q.full; p.S = q.S;
+    const int64_t sliced = q.S > 1 ? (q.total - q.full) * q.S : 0;
     constexpr int lds = 2 * 4 * T * 64;
     auto kern = ns_product_kernel<E, P, T>;
     if (lds > 65536) {
@@ -789,12 +860,12 @@ static void ns_product(NsArgs p, int64_t rows, int64_t cols, int S, hipStream_t 
       (void)hipGetLastError();
     }
     const char* name = P == NS_GRAM ? "ns_product_kernel (X X^T)" : P == NS_POLY ? "ns_product_kernel (Q)" : "ns_product_kernel (Q X)";
-    DMOE_LAUNCH_NAMED(name, kern, dim3((unsigned)((total + 7) / 8 * 8)), dim3(T == 256 ? 512 : 256), lds, st, p);
-    if constexpr (P == NS_GRAM && T == 128)
-      if (S > 1)
-        DMOE_LAUNCH_NAMED("ns_finish_kernel", ns_finish_kernel<T>, dim3((unsigned)(p.groups * p.tiles * 16)), dim3(64), 0, st, p);
+    DMOE_LAUNCH_NAMED(name, kern, dim3((unsigned)(q.full + (sliced + 7) / 8 * 8)), dim3(T == 256 ? 512 : 256), lds, st, p);
+    if (sliced)
+      DMOE_LAUNCH_NAMED("ns_finish_kernel", (ns_finish_kernel<E, P, T>), dim3((unsigned)((q.total - q.full) * (T / 32) * (T / 32))),
+                        dim3(64), 0, st, p);
   };
-  if (whole && S == 1 && t256 <= t128) go(std::integral_constant<int, 256>{});
+  if (q.T == 256) go(std::integral_constant<int, 256>{});
   else go(std::integral_constant<int, 128>{});
 }
 
@@ -826,19 +897,19 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     for (int k = 0; k < q.steps; ++k) {
       const int x = k & 1;
       NsArgs p{};
-      p.groups = g; p.e0 = (int)e0; p.u = u;
-      p.part = o.S > 1 ? reinterpret_cast<float*>(ws + o.sums) : nullptr;
+      p.e0 = (int)e0; p.u = u;
+      p.part = reinterpret_cast<float*>(ws + o.sums);
       p.Ah = p.Bh = f(o.xh[x]); p.Al = p.Bl = f(o.xl[x]); p.lda = p.ldb = Cp; p.sa = p.sb = sx; p.K = Cp;
       p.Ch = f(o.ah); p.Cl = f(o.al); p.ldc = Rp; p.sc = sr;
-      ns_product<E, NS_GRAM>(p, o.Rp, o.Rp, o.S, st);
+      ns_product<float, NS_GRAM>(p, g, o.Rp, o.Rp, st);
       p.Ah = p.Bh = f(o.ah); p.Al = p.Bl = f(o.al); p.lda = p.ldb = Rp; p.sa = p.sb = sr; p.K = Rp;
       p.Ch = f(o.qh); p.Cl = f(o.ql);
-      ns_product<E, NS_POLY>(p, o.Rp, o.Rp, 1, st);
+      ns_product<float, NS_POLY>(p, g, o.Rp, o.Rp, st);
       p.Ah = f(o.qh); p.Al = f(o.ql);
       p.Bh = f(o.xh[x]); p.Bl = f(o.xl[x]); p.ldb = Cp; p.sb = sx;
       p.Ch = f(o.xh[x ^ 1]); p.Cl = f(o.xl[x ^ 1]); p.ldc = Cp; p.sc = sx;
-      if (k + 1 < q.steps) ns_product<E, NS_APPLY>(p, o.Rp, o.Cp, 1, st);
-      else ns_product<E, NS_LAST>(p, o.Rp, o.Cp, 1, st);
+      if (k + 1 < q.steps) ns_product<float, NS_APPLY>(p, g, o.Rp, o.Cp, st);
+      else ns_product<E, NS_LAST>(p, g, o.Rp, o.Cp, st);
     }
   }
 }

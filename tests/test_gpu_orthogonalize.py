@@ -105,9 +105,10 @@ def test_short_side_above_64(shape, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("shape", [(16, 1024, 1024), (15, 1021, 1279), (12, 1279, 1021), (130, 1024, 1024)], ids=str)
+@pytest.mark.parametrize("shape", [(16, 1024, 1024), (15, 1021, 1279), (12, 1279, 1021), (130, 1024, 1024), (2, 2048, 2048),
+                                   (1, 4096, 1100), (1, 1100, 4096), (9, 1024, 1024), (5, 1536, 1280), (1, 2304, 2304)], ids=str)
 def test_large_tiles_and_groups(shape):
-    """Enough work for 256 x 256 tiles, and (130 matrices) more than one group."""
+    """Work for 256 x 256 tiles, whole and sliced last rounds, and (130 matrices) more than one group."""
     G = _make(*shape, "f32", 5)
     out = _call(G)
     for i in range(0, shape[0], 13):
