@@ -13,7 +13,16 @@
 // values stay below 1.21, A's below 1.45, and a I + b A + c A A lies between 0.6 and a), and
 // three products hi hi + hi lo + lo hi into one fp32 accumulator.  A and Q = a I + b A + c A A are
 // symmetric: tiles of the lower triangle only, stored twice.  Bound by the fp16 matrix rate:
-// 3 (r^2 c + r^3 + 2 r^2 c) multiply-adds' flops a step.
+// 3 (r^2 c + r^3 + 2 r^2 c) flops for a single step.
+//
+// Several steps share a pass over X: with P = Q_k .. Q_1 and A_(k+1) = Q_k A_k Q_k, all polynomials of
+// the first A and so symmetric, X <- P X.  Every further step costs four symmetric products of r^3 in
+// place of one, X X^T and Q X.  The price is that A_k is no longer formed from a rounded X: what
+// rounding leaves in A grows by a^2 a step.  Two steps to a pass have the error of single steps or
+// less (1.8e-6 to 5e-5 of the result, as plain fp32; simulated spectra: full rank, ranks 8 to 256 with
+// and without noise, one to eight dominant directions, powers), five 2e-6 to 4e-4: fp32 takes two and
+// bf16, which rounds the result by 1.7e-3, five, where that is the shorter by the estimates of
+// ns_tiling.
 //
 // r <= 64: everything in the r x r space in fp64.  X_k = P_k X_0 with P_k a polynomial of
 // A_0 = X_0 X_0^T, so  Q = a I + b A + c A A,  P <- Q P,  A <- Q A Q  from A_0, P_0 = I, and
@@ -38,6 +47,7 @@ constexpr double NS_EPS = 1e-7;
 constexpr float SPLIT = 16384.f;          // operands are held as value * SPLIT = hi + lo
 constexpr int64_t ORTHO_MAX = 32768;      // largest m, n
 constexpr int64_t GRAM_R = 64;            // largest r of the fp64 route
+constexpr int NS_MERGE_BF16 = 5, NS_MERGE_F32 = 2;     // most steps to a pass over X
 
 // What the update is made of.
 struct UpdateArgs {
@@ -78,15 +88,14 @@ __device__ __forceinline__ void store_at(const UpdateArgs& a, int64_t at, float 
   *p = cvt<E>(a.mom ? fmaf(-a.lr, o, a.keep * ldf(p)) : o);
 }
 
-constexpr float NS_DOWN = 1.f / (SPLIT * SPLIT);      // of a product of two operands
 // The same for 16 bytes of a row, from accumulators.
 template <typename E>
-__device__ __forceinline__ void store_row(const UpdateArgs& a, int64_t at, float (&o)[Vec<E>::N]) {
+__device__ __forceinline__ void store_row(const UpdateArgs& a, int64_t at, float down, float (&o)[Vec<E>::N]) {
   uint4* p = reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.out) + at);
   float w[Vec<E>::N];
   if (a.mom) Vec<E>::unpack(*p, w);
 #pragma unroll
-  for (int i = 0; i < Vec<E>::N; ++i) o[i] = a.mom ? fmaf(-a.lr, o[i] * NS_DOWN, a.keep * w[i]) : o[i] * NS_DOWN;
+  for (int i = 0; i < Vec<E>::N; ++i) o[i] = a.mom ? fmaf(-a.lr, o[i] * down, a.keep * w[i]) : o[i] * down;
   *p = Vec<E>::pack(o);
 }
 
@@ -271,9 +280,9 @@ __device__ __forceinline__ void stage_sync() {
 }
 
 enum NsProduct {
-  NS_GRAM,    // A = X X^T
-  NS_POLY,    // Q = a I + b A + c A A
-  NS_APPLY,   // X' = Q X
+  NS_SYM,     // a symmetric product: X X^T, or two polynomials of the same A
+  NS_POLY,    // a I + b A + c A A
+  NS_APPLY,   // X' = P X
   NS_LAST     // the same, into O or the parameters
 };
 
@@ -285,6 +294,7 @@ struct NsArgs {
   int TI, tiles, total;                   // rows of tiles, tiles of a matrix and of all
   int full, S;                            // tiles past `full` are split into S slices of the contraction:
   float* part;                            // their sums
+  float down;                             // result (its scale included) over accumulator
   int e0;                                 // first matrix
   UpdateArgs u;
 };
@@ -295,7 +305,7 @@ __device__ __forceinline__ int xcd_run(int b, int count) { return (b & 7) * (cou
 // Tile t of a matrix: row ti, column tj.  Symmetric results: the lower triangle, row by row.
 template <int P>
 __device__ __forceinline__ void tile_at(const NsArgs& p, int t, int& ti, int& tj) {
-  if constexpr (P == NS_GRAM || P == NS_POLY) {
+  if constexpr (P == NS_SYM || P == NS_POLY) {
     ti = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
     while (ti * (ti + 1) / 2 > t) --ti;
     while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
@@ -306,12 +316,11 @@ __device__ __forceinline__ void tile_at(const NsArgs& p, int t, int& ti, int& tj
   }
 }
 
-// The value of a symmetric result from its accumulator (2^28 times the product).
+// A result, at its scale, from its accumulator.
 template <int P>
-__device__ __forceinline__ float ns_value(float acc, float ah, float al, int i, int j) {
-  constexpr float D = 1.f / SPLIT;
-  if constexpr (P == NS_POLY) return (float)NS_C * (acc * D) + (float)NS_B * (ah + al) + (i == j ? (float)NS_A * SPLIT : 0.f);
-  else return acc * D;
+__device__ __forceinline__ float ns_value(float acc, float down, float ah, float al, int i, int j) {
+  if constexpr (P == NS_POLY) return (float)NS_C * (acc * down) + (float)NS_B * (ah + al) + (i == j ? (float)NS_A * SPLIT : 0.f);
+  else return acc * down;
 }
 
 // One T x T tile to a block (8 waves of 128 x 64 for T = 256, 4 of 64 x 64 for 128): two LDS stages
@@ -321,7 +330,7 @@ __global__ void __launch_bounds__(T == 256 ? 512 : 256)
 ns_product_kernel(NsArgs p) {
   constexpr int WM = 2, WN = T / 64, NW = WM * WN;
   constexpr int TM = T / WM / 32, TN = 2;
-  constexpr bool SYM = P == NS_GRAM || P == NS_POLY;
+  constexpr bool SYM = P == NS_SYM || P == NS_POLY;
   using TA = RowTile<T, NW>;
   using TB = typename std::conditional<SYM, RowTile<T, NW>, ColTile<T, NW>>::type;
   constexpr int STAGE = 2 * TA::BYTES + 2 * TB::BYTES;
@@ -450,13 +459,13 @@ ns_product_kernel(NsArgs p) {
             float o[V];
 #pragma unroll
             for (int x = 0; x < V; x += 4) *reinterpret_cast<float4*>(o + x) = *reinterpret_cast<const float4*>(buf + r * 36 + c + x);
-            if (row0 + r < p.u.m && col0 + c < p.u.n) store_row<E>(p.u, base + (int64_t)(row0 + r) * p.u.n + col0 + c, o);
+            if (row0 + r < p.u.m && col0 + c < p.u.n) store_row<E>(p.u, base + (int64_t)(row0 + r) * p.u.n + col0 + c, p.down, o);
           }
         } else {
 #pragma unroll 4
           for (int q = lane >> 5; q < 32; q += 2) {
             const int row = row0 + q, col = col0 + lp;
-            if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + (int64_t)row * p.u.n + col, buf[q * 36 + lp] * NS_DOWN);
+            if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + (int64_t)row * p.u.n + col, buf[q * 36 + lp] * p.down);
           }
         }
         wave_sync();
@@ -484,7 +493,7 @@ ns_product_kernel(NsArgs p) {
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float val = ns_value<P>(acc[i][j][v + q], (float)h4[q], (float)l4[q], row, col + q);
+          const float val = ns_value<P>(acc[i][j][v + q], p.down, (float)h4[q], (float)l4[q], row, col + q);
           acc[i][j][v + q] = val;
           f16 vh, vl;
           split(val, vh, vl);
@@ -566,7 +575,7 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int col = col0 + 8 * v + q;
-        if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + col, acc[v][q] * NS_DOWN);
+        if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + col, acc[v][q] * p.down);
       }
   } else {
     f16* Ch = p.Ch + g * p.sc;
@@ -583,9 +592,9 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         f16 vh, vl;
-        split(ns_value<P>(acc[v][q], (float)h4[q], (float)l4[q], row, col + q), vh, vl);
+        split(ns_value<P>(acc[v][q], p.down, (float)h4[q], (float)l4[q], row, col + q), vh, vl);
         h[q] = vh; l[q] = vl;
-        if ((P == NS_GRAM || P == NS_POLY) && ti != tj) {
+        if ((P == NS_SYM || P == NS_POLY) && ti != tj) {
           Ch[(int64_t)(col + q) * p.ldc + row] = vh;
           Cl[(int64_t)(col + q) * p.ldc + row] = vl;
         }
@@ -767,7 +776,7 @@ __global__ void __launch_bounds__(GR_NT) gram_apply_kernel(UpdateArgs a, const d
 
 // How a product of `groups` matrices is cut: T x T tiles, the tiles past `full` with their contraction
 // in S slices.
-struct NsTiling { int T, S; int64_t tiles, full, total; };
+struct NsTiling { int T, S; int64_t tiles, full, total; double us; };
 
 // 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one.  A round of them takes
 // 2.53 / 1.54 us per 32 of the contraction (measured at K = 4096 and 16384), 1.07 where the smaller
@@ -789,7 +798,7 @@ static NsTiling ns_tiling(int64_t groups, bool sym, int64_t rows, int64_t cols, 
                        (S > 1 ? 12.0 + (double)(blocks * T * T * 8) / 5e6 : 0.0);
       if (!best.T || t < least) {
         least = t;
-        best = NsTiling{T, S, tiles, S > 1 ? total - rem : (total + 7) / 8 * 8, total};
+        best = NsTiling{T, S, tiles, S > 1 ? total - rem : (total + 7) / 8 * 8, total, t + 5.0};
       }
     }
   }
@@ -801,7 +810,8 @@ struct OrthoPlan {
   int64_t r, c, Rp, Cp;
   int group;                              // matrices at a time
   int slices, nb;                         // fp64 route's slices; blocks of the norm
-  size_t part, P, xh[2], xl[2], ah, al, qh, ql, sums, total;
+  int merge;                              // steps to one pass over X
+  size_t part, P, xh[2], xl[2], sh[6], sl[6], sums, total;   // r x r: A, A Q, two of Q, two of their products
 };
 
 static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
@@ -834,7 +844,14 @@ static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
   const size_t g = (size_t)o->group;
   o->part = off; off += up(g * NB_MAX * sizeof(double));
   for (size_t* p : {&o->xh[0], &o->xl[0], &o->xh[1], &o->xl[1]}) { *p = off; off += up(g * o->Rp * o->Cp * 2); }
-  for (size_t* p : {&o->ah, &o->al, &o->qh, &o->ql}) { *p = off; off += up(g * o->Rp * o->Rp * 2); }
+  // Steps to one pass over X (see the top): estimated, the fewest passes against none saved.
+  const NsTiling gram = ns_tiling(o->group, true, o->Rp, o->Rp, o->Cp), sym = ns_tiling(o->group, true, o->Rp, o->Rp, o->Rp),
+                 apply = ns_tiling(o->group, false, o->Rp, o->Cp, o->Rp);
+  const int most = std::min<int>(q->steps, q->dtype == DMOE_BF16 ? NS_MERGE_BF16 : NS_MERGE_F32);
+  const double one = gram.us + sym.us + apply.us, many = gram.us + (4 * most - 3) * sym.us + apply.us;
+  o->merge = many < most * one ? most : 1;
+  for (int i = 0; i < (o->merge > 1 ? 6 : 3); ++i)
+    for (size_t* p : {&o->sh[i], &o->sl[i]}) { *p = off; off += up(g * o->Rp * o->Rp * 2); }
   size_t sums = 0;
   for (int64_t k : {(int64_t)o->group, q->B % o->group})          // whole groups and the last one
     for (const NsTiling& t : {ns_tiling(k, true, o->Rp, o->Rp, o->Cp), ns_tiling(k, true, o->Rp, o->Rp, o->Rp),
@@ -848,7 +865,7 @@ static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
 // E: the type of the result of NS_LAST
 template <typename E, int P>
 static void ns_product(NsArgs p, int64_t groups, int64_t rows, int64_t cols, hipStream_t st) {
-  const NsTiling q = ns_tiling(groups, P == NS_GRAM || P == NS_POLY, rows, cols, p.K);
+  const NsTiling q = ns_tiling(groups, P == NS_SYM || P == NS_POLY, rows, cols, p.K);
   auto go = [&](auto Tc) {
     constexpr int T = decltype(Tc)::value;
     p.TI = (int)(rows / T); p.tiles = (int)q.tiles; p.total = (int)q.total; p.full = (int)q.full; p.S = q.S;
@@ -859,7 +876,7 @@ static void ns_product(NsArgs p, int64_t groups, int64_t rows, int64_t cols, hip
       (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       (void)hipGetLastError();
     }
-    const char* name = P == NS_GRAM ? "ns_product_kernel (X X^T)" : P == NS_POLY ? "ns_product_kernel (Q)" : "ns_product_kernel (Q X)";
+    const char* name = P == NS_SYM ? "ns_product_kernel (symmetric)" : P == NS_POLY ? "ns_product_kernel (Q)" : "ns_product_kernel (P X)";
     DMOE_LAUNCH_NAMED(name, kern, dim3((unsigned)(q.full + (sliced + 7) / 8 * 8)), dim3(T == 256 ? 512 : 256), lds, st, p);
     if (sliced)
       DMOE_LAUNCH_NAMED("ns_finish_kernel", (ns_finish_kernel<E, P, T>), dim3((unsigned)((q.total - q.full) * (T / 32) * (T / 32))),
@@ -894,22 +911,54 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     DMOE_LAUNCH_NAMED("ortho_norm_kernel", norm, dim3(o.nb, g), dim3(256), 0, st, u, (int)e0, part);
     DMOE_LAUNCH_NAMED("ortho_split_kernel", ortho_split_kernel<E>, dim3(Cp / 64, Rp / 64, g), dim3(256), 0, st, u, (int)e0, part,
                       o.nb, f(o.xh[0]), f(o.xl[0]), Rp, Cp, sx);
-    for (int k = 0; k < q.steps; ++k) {
-      const int x = k & 1;
-      NsArgs p{};
-      p.e0 = (int)e0; p.u = u;
-      p.part = reinterpret_cast<float*>(ws + o.sums);
+    NsArgs p{};
+    p.e0 = (int)e0; p.u = u;
+    p.part = reinterpret_cast<float*>(ws + o.sums);
+    enum { A = 0, AQ = 1, Q0 = 2, P0 = 4 };
+    auto left = [&](int i) { p.Ah = f(o.sh[i]); p.Al = f(o.sl[i]); p.lda = Rp; p.sa = sr; };
+    auto right = [&](int i) { p.Bh = f(o.sh[i]); p.Bl = f(o.sl[i]); p.ldb = Rp; p.sb = sr; };
+    auto to = [&](int i) { p.Ch = f(o.sh[i]); p.Cl = f(o.sl[i]); p.ldc = Rp; p.sc = sr; };
+    int x = 0;
+    for (int k = 0; k < q.steps;) {
+      const int merge = std::min(o.merge, q.steps - k);
       p.Ah = p.Bh = f(o.xh[x]); p.Al = p.Bl = f(o.xl[x]); p.lda = p.ldb = Cp; p.sa = p.sb = sx; p.K = Cp;
-      p.Ch = f(o.ah); p.Cl = f(o.al); p.ldc = Rp; p.sc = sr;
-      ns_product<float, NS_GRAM>(p, g, o.Rp, o.Rp, st);
-      p.Ah = p.Bh = f(o.ah); p.Al = p.Bl = f(o.al); p.lda = p.ldb = Rp; p.sa = p.sb = sr; p.K = Rp;
-      p.Ch = f(o.qh); p.Cl = f(o.ql);
-      ns_product<float, NS_POLY>(p, g, o.Rp, o.Rp, st);
-      p.Ah = f(o.qh); p.Al = f(o.ql);
+      to(A);
+      p.down = 1.f / SPLIT;
+      ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
+      p.K = Rp;
+      int P = -1;                          // the steps' product so far, held at SPLIT / 4^(steps - 1)
+      float up = 1.f;
+      for (int i = 0; i < merge; ++i) {
+        const int Q = Q0 + (i & 1);
+        left(A); right(A); to(Q);
+        p.down = 1.f / SPLIT;
+        ns_product<float, NS_POLY>(p, g, o.Rp, o.Rp, st);
+        if (i == 0) {
+          P = Q;
+        } else {
+          left(Q); right(P);
+          P = P0 + (i & 1);
+          to(P);
+          p.down = 0.25f / SPLIT;
+          ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
+          up *= 4.f;
+        }
+        if (i + 1 < merge) {               // A of the next step
+          p.down = 1.f / SPLIT;
+          left(Q); right(A); to(AQ);
+          ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
+          left(AQ); right(Q); to(A);
+          ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
+        }
+      }
+      k += merge;
+      left(P);
       p.Bh = f(o.xh[x]); p.Bl = f(o.xl[x]); p.ldb = Cp; p.sb = sx;
       p.Ch = f(o.xh[x ^ 1]); p.Cl = f(o.xl[x ^ 1]); p.ldc = Cp; p.sc = sx;
-      if (k + 1 < q.steps) ns_product<float, NS_APPLY>(p, g, o.Rp, o.Cp, st);
+      p.down = (k < q.steps ? 1.f / SPLIT : 1.f / (SPLIT * SPLIT)) * up;
+      if (k < q.steps) ns_product<float, NS_APPLY>(p, g, o.Rp, o.Cp, st);
       else ns_product<E, NS_LAST>(p, g, o.Rp, o.Cp, st);
+      x ^= 1;
     }
   }
 }
