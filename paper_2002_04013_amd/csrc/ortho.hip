@@ -166,8 +166,8 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
 }
 
 // X (hi and lo planes [Rp][Cp]) = U / (|U| + eps), padded with zeros; a block to a 64 x 64 piece,
-// turned through LDS where m > n.
-template <typename E>
+// turned through LDS where m > n.  WIDE: 16 bytes of G to a thread (n a multiple of them).
+template <typename E, bool WIDE>
 __global__ void __launch_bounds__(256)
 ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* hi, f16* lo, int Rp, int Cp, int64_t plane) {
   __shared__ float tile[64][65];
@@ -184,6 +184,35 @@ ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* hi, f1
   const int x0 = blockIdx.x * 64, y0 = blockIdx.y * 64;            // column and row of X
   const int i0 = turn ? x0 : y0, j0 = turn ? y0 : x0;              // of U
   const int64_t base = (int64_t)e * a.m * a.n;
+  if constexpr (WIDE) {
+    constexpr int V = Vec<E>::N, LPR = 64 / V, N = 64 * 64 / V / 256;
+    uint4 gq[N];
+    float4 mq[N][V / 4];
+    // all of the thread's loads first
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int q = threadIdx.x + 256 * k, i = i0 + q / LPR, j = j0 + q % LPR * V;
+      const bool ok = i < a.m && j < a.n;
+      const int64_t at = base + (int64_t)i * a.n + j;
+      gq[k] = ok ? *reinterpret_cast<const uint4*>(reinterpret_cast<const E*>(a.G) + at) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < V / 4; ++x)
+        mq[k][x] = ok && a.mom ? *reinterpret_cast<const float4*>(a.mom + at + 4 * x) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int q = threadIdx.x + 256 * k;
+      float u[V];
+      Vec<E>::unpack(gq[k], u);
+#pragma unroll
+      for (int x = 0; x < V; ++x) {
+        const float4 m4 = mq[k][x / 4];
+        const float m = x % 4 == 0 ? m4.x : x % 4 == 1 ? m4.y : x % 4 == 2 ? m4.z : m4.w;
+        if (a.mom) u[x] = a.nesterov ? fmaf(a.mu, m, u[x]) : m;
+        tile[q / LPR][q % LPR * V + x] = u[x];
+      }
+    }
+  } else
   for (int q = threadIdx.x; q < 64 * 64; q += 8 * 256) {
     int64_t at[8];
     bool ok[8];
@@ -274,9 +303,10 @@ struct ColTile {
 // Orders the LDS operations of one wave for the compiler; the hardware keeps their order.
 __device__ __forceinline__ void wave_sync() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// Every load of this wave has landed and its LDS reads are done, for the whole block.
+// All but the newest N loads of this wave have landed and its LDS reads are done, for the whole block.
+template <int N>
 __device__ __forceinline__ void stage_sync() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 enum NsProduct {
@@ -323,12 +353,17 @@ __device__ __forceinline__ float ns_value(float acc, float down, float ah, float
   else return acc * down;
 }
 
-// One T x T tile to a block (8 waves of 128 x 64 for T = 256, 4 of 64 x 64 for 128): two LDS stages
-// of 32, the next one loaded while the current one is multiplied.
+// One T x T tile to a block (8 waves of 128 x 64 for T = 256, 4 of 64 x 64 for 128): two LDS stages of
+// 32, the next one loading while the current one is multiplied.  A CU's LDS moves 128 bytes a
+// cycle: 2048 cycles of reads and loads to 3072 of products for T = 256, as many as of products for 128,
+// two blocks to a unit.  MFMAs are busy 70% of the time at T = 256, at 1.6 GHz (the clock the power
+// limit leaves): 1273 TFLOP/s of fp16 products at r = 4096, c = 16384, where a library product of
+// 8192 x 8192 runs at 1470.  Four stages for T = 128 (a block to a unit): 1 to 10% slower.
 template <typename E, int P, int T>
 __global__ void __launch_bounds__(T == 256 ? 512 : 256)
 ns_product_kernel(NsArgs p) {
   constexpr int WM = 2, WN = T / 64, NW = WM * WN;
+  constexpr bool PIPE = T == 128;          // see run(); 256 x 256 tiles have two waves to a SIMD that cover each other
   constexpr int TM = T / WM / 32, TN = 2;
   constexpr bool SYM = P == NS_SYM || P == NS_POLY;
   using TA = RowTile<T, NW>;
@@ -370,43 +405,75 @@ ns_product_kernel(NsArgs p) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
+  // operands of 16 of the contraction
+  struct Frags { f16x8_t ah[TM], al[TM], bh[TN], bl[TN]; };
+  auto read = [&](Frags& f, int k, int kk) {
+    const char* st = smem + (k & 1) * STAGE;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int c0 = wn * 64 + j * 32;
+      f.bh[j] = TB::frag(st + 2 * TA::BYTES, c0, kk, lane);
+      f.bl[j] = TB::frag(st + 2 * TA::BYTES + TB::BYTES, c0, kk, lane);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int r0 = wm * (T / WM) + i * 32;
+      f.ah[i] = TA::frag(st, r0, kk, lane);
+      f.al[i] = TA::frag(st + TA::BYTES, r0, kk, lane);
+    }
+  };
   auto run = [&](auto TURN) {
-    load(0);
-    for (int k = 0; k < nk; ++k) {
-      stage_sync();
-      if (k + 1 < nk) load(k + 1);
-      const char* st = smem + (k & 1) * STAGE;
+    auto mma = [&](const f16x8_t& a, const f16x8_t& b, f32x16_t c) {
+      if constexpr (TURN.value) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+      else return __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, c, 0, 0, 0);
+    };
+    auto multiply = [&](const Frags& f) {
 #pragma unroll
-      for (int kk = 0; kk < NS_BK; kk += 16) {
-        f16x8_t ah[TM], al[TM], bh[TN], bl[TN];
+      for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const int c0 = wn * 64 + j * 32;
-          bh[j] = TB::frag(st + 2 * TA::BYTES, c0, kk, lane);
-          bl[j] = TB::frag(st + 2 * TA::BYTES + TB::BYTES, c0, kk, lane);
+        for (int j = 0; j < TN; ++j) acc[i][j] = mma(f.ah[i], f.bl[j], acc[i][j]);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mma(f.al[i], f.bh[j], acc[i][j]);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mma(f.ah[i], f.bh[j], acc[i][j]);
+    };
+    constexpr int LPS = 2 * (TA::PER_WAVE + TB::PER_WAVE);           // loads of a stage, per wave
+    if constexpr (PIPE) {
+      // The second half's operands are read before the first half's products, and the next
+      // stage's first operands before the second half's, which cover the reads.
+      load(0);
+      if (nk > 1) load(1);
+      if (nk > 1) stage_sync<LPS>();
+      else stage_sync<0>();
+      Frags f0, f1;
+      read(f0, 0, 0);
+      for (int k = 0; k < nk; ++k) {
+        read(f1, k, 16);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(f0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (k + 1 < nk) {
+          stage_sync<0>();
+          if (k + 2 < nk) load(k + 2);
+          read(f0, k + 1, 0);
         }
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const int r0 = wm * (T / WM) + i * 32;
-          ah[i] = TA::frag(st, r0, kk, lane);
-          al[i] = TA::frag(st + TA::BYTES, r0, kk, lane);
-        }
-        auto mma = [&](const f16x8_t& a, const f16x8_t& b, f32x16_t c) {
-          if constexpr (TURN.value) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-          else return __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, c, 0, 0, 0);
-        };
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = mma(ah[i], bl[j], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = mma(al[i], bh[j], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = mma(ah[i], bh[j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(f1);
+      }
+    } else {
+      load(0);
+      for (int k = 0; k < nk; ++k) {
+        stage_sync<0>();
+        if (k + 1 < nk) load(k + 1);
+        Frags f;
+        read(f, k, 0);
+        multiply(f);
+        read(f, k, 16);
+        multiply(f);
       }
     }
   };
@@ -433,7 +500,7 @@ ns_product_kernel(NsArgs p) {
               make_float4(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
     return;
   }
-  stage_sync();                              // the ring is free: 16 KiB of it to a wave
+  stage_sync<0>();                           // the ring is free: 16 KiB of it to a wave
   char* mine = smem + wave * 16384;
 
   if constexpr (P == NS_LAST) {
@@ -778,28 +845,25 @@ __global__ void __launch_bounds__(GR_NT) gram_apply_kernel(UpdateArgs a, const d
 // in S slices.
 struct NsTiling { int T, S; int64_t tiles, full, total; double us; };
 
-// 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one.  A round of them takes
-// 2.53 / 1.54 us per 32 of the contraction (measured at K = 4096 and 16384), 1.07 where the smaller
-// ones have a unit to themselves; what a last, partly filled round would take is shortened by
-// slices, at the price of a second launch and the slices' sums through memory (10 to 20 us).
+// 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one.  Measured, us per round of
+// tiles: 2.45 / 1.65 per 32 of the contraction, 0.85 where the smaller ones have a unit to
+// themselves, and the tiles' stores (a symmetric result's twice over).  What a last, partly filled round
+// would take is shortened by slices, at the price of a second launch and the slices' sums
+// through memory (10 to 20 us).
 static NsTiling ns_tiling(int64_t groups, bool sym, int64_t rows, int64_t cols, int64_t K) {
   NsTiling best{};
-  double least = 0.0;
   const int64_t k = K / NS_BK;
   for (int T : {256, 128}) {
     if (rows % T || cols % T) continue;
     const int64_t a = rows / T, b = cols / T, slots = T == 256 ? 256 : 512;
     const int64_t tiles = sym ? a * (a + 1) / 2 : a * b, total = groups * tiles, rem = total % slots;
-    const double c = T == 256 ? 2.53 : 1.54, alone = T == 256 ? 2.53 : 1.07;
+    const double c = T == 256 ? 2.45 : 1.65, alone = T == 256 ? 2.45 : 0.85, store = T == 256 ? (sym ? 20.0 : 8.0) : (sym ? 3.0 : 2.0);
     for (int S = 1; S <= 32 && (S == 1 || (rem && k >= 8 * S)); ++S) {
       const int64_t blocks = rem * S, last = blocks % slots;
       const double rounds = (double)(blocks / slots) * c + (last == 0 ? 0.0 : last <= 256 ? alone : c);
-      const double t = (double)(total / slots * k) * c + rounds * (double)((k + S - 1) / S) +
-                       (S > 1 ? 12.0 + (double)(blocks * T * T * 8) / 5e6 : 0.0);
-      if (!best.T || t < least) {
-        least = t;
-        best = NsTiling{T, S, tiles, S > 1 ? total - rem : (total + 7) / 8 * 8, total, t + 5.0};
-      }
+      const double us = (double)(total / slots) * ((double)k * c + store) + rounds * (double)((k + S - 1) / S) +
+                        (S > 1 ? 9.0 + (double)(blocks * T * T * 8) / 5e6 : rem ? store : 0.0) + 2.0;
+      if (!best.T || us < best.us) best = NsTiling{T, S, tiles, S > 1 ? total - rem : (total + 7) / 8 * 8, total, us};
     }
   }
   return best;
@@ -909,7 +973,8 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     const bool wide = q.m * q.n % Vec<E>::N == 0;
     auto norm = wide ? ortho_norm_kernel<E, true> : ortho_norm_kernel<E, false>;
     DMOE_LAUNCH_NAMED("ortho_norm_kernel", norm, dim3(o.nb, g), dim3(256), 0, st, u, (int)e0, part);
-    DMOE_LAUNCH_NAMED("ortho_split_kernel", ortho_split_kernel<E>, dim3(Cp / 64, Rp / 64, g), dim3(256), 0, st, u, (int)e0, part,
+    auto planes = q.n % Vec<E>::N == 0 ? ortho_split_kernel<E, true> : ortho_split_kernel<E, false>;
+    DMOE_LAUNCH_NAMED("ortho_split_kernel", planes, dim3(Cp / 64, Rp / 64, g), dim3(256), 0, st, u, (int)e0, part,
                       o.nb, f(o.xh[0]), f(o.xl[0]), Rp, Cp, sx);
     NsArgs p{};
     p.e0 = (int)e0; p.u = u;
