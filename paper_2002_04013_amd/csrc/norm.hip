@@ -22,17 +22,20 @@ constexpr int64_t LNORM_DMAX = 16384;    // widest row: 1024 lanes of four fp32 
 constexpr int lnorm_threads(int GS) { return GS > 256 ? GS : 256; }
 
 // Lanes and chunks of a row of `nch` chunks (at most 2048 in bf16, 4096 in fp32): a lane to a
-// chunk up to a wave, then up to four chunks to a lane of one wave (no barrier), then of four
-// to sixteen waves.
+// chunk up to a wave, two up to two waves' worth.  Wider rows: the forward has up to four chunks to a lane
+// of one wave (no barrier), then of four to sixteen waves; the backward, whose column sums take
+// 2 VEC registers to a chunk, at most two up to 1024 chunks (8192 rows x 4096 fp32 118 -> 106 us, 8000 x 8192
+// bf16 158 -> 118 with four a lane / two; 4000 x 16384 bf16 179 with four, 252 with two).
 struct RowShape { int gs, ch; };
-static RowShape row_shape(int64_t nch) {
+static RowShape row_shape(int64_t nch, bool bwd) {
   for (int gs = 8; gs <= 64; gs *= 2)
     if (nch <= gs) return {gs, 1};
   if (nch <= 64 * 2) return {64, 2};
-  if (nch <= 64 * 4) return {64, 4};
+  if (nch <= 64 * 4) return bwd ? RowShape{256, 1} : RowShape{64, 4};
   if (nch <= 256 * 2) return {256, 2};
-  if (nch <= 256 * 4) return {256, 4};
-  return {nch <= 512 * 4 ? 512 : 1024, 4};
+  if (nch <= 256 * 4) return bwd ? RowShape{512, 2} : RowShape{256, 4};
+  if (nch <= 512 * 4) return {512, 4};
+  return {1024, 4};
 }
 
 // Sum over the GS lanes of a row.  `red`: two slots of 16 floats per sum, taken in turn: a
@@ -263,37 +266,45 @@ layer_norm_bwd_kernel(const E* s, const float* stats, const E* gamma, const E* d
   }
 }
 
-// dgamma, dbeta = the nb blocks' sums in block order.  A block takes LR_C columns of the 2 D;
-// slice threadIdx / LR_C of it adds a contiguous run of the blocks, the slices meet in LDS.
-constexpr int LR_NT = 512, LR_C = 16, LR_S = LR_NT / LR_C;
+// dgamma, dbeta = the nb blocks' sums in block order.  A block takes 32 of the 2 D columns, 16 bytes
+// to a thread (128-byte pieces of the sums); slice threadIdx / LR_C adds a contiguous run of the
+// blocks, the slices meet in LDS.
+constexpr int LR_NT = 512, LR_C = 8, LR_S = LR_NT / LR_C;
 template <typename E>
 __global__ void __launch_bounds__(LR_NT)
 layer_norm_reduce_kernel(const float* part, int nb, int D, E* dgamma, E* dbeta) {
-  __shared__ float sums[LR_S][LR_C + 1];
+  __shared__ float4 sums[LR_S][LR_C + 1];
   const int cc = threadIdx.x % LR_C, sl = threadIdx.x / LR_C;
-  const int64_t c = (int64_t)blockIdx.x * LR_C + cc;            // 2 D is a multiple of LR_C
+  const int64_t c = ((int64_t)blockIdx.x * LR_C + cc) * 4;      // 2 D is a multiple of 128
   const int per = (nb + LR_S - 1) / LR_S;
   const int b1 = min(nb, (sl + 1) * per);
-  float t = 0.f;
+  float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& v) { t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w; };
 #pragma unroll 8
-  for (int b = sl * per; b < b1; ++b) t += part[(int64_t)b * 2 * D + c];
+  for (int b = sl * per; b < b1; ++b) add(*reinterpret_cast<const float4*>(part + (int64_t)b * 2 * D + c));
   sums[sl][cc] = t;
   __syncthreads();
-  if (sl) return;
-  for (int i = 1; i < LR_S; ++i) t += sums[i][cc];
-  if (c < D) dgamma[c] = cvt<E>(t);
-  else if (dbeta) dbeta[c - D] = cvt<E>(t);
+  if (threadIdx.x >= 4 * LR_C) return;
+  // a thread to a column
+  const int q = threadIdx.x;
+  float s = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < LR_S; ++i) s += reinterpret_cast<const float*>(&sums[i][0])[q];
+  const int64_t o = (int64_t)blockIdx.x * LR_C * 4 + q;
+  if (o < D) dgamma[o] = cvt<E>(s);
+  else if (dbeta) dbeta[o - D] = cvt<E>(s);
 }
 
-// Blocks of the backward: four to a compute unit, each at least one row per group.
+// Blocks of the backward: as many as stay resident (three of 256 threads to a compute unit), each at
+// least one row per group; more would only add sums for the second kernel.
 static int64_t lnorm_bwd_blocks(const Shape& s) {
-  const RowShape q = row_shape(s.D * (int64_t)s.esz / 16);
-  const int64_t groups = lnorm_threads(q.gs) / q.gs;
-  return std::min<int64_t>((s.T + groups - 1) / groups, q.gs > 256 ? 512 : 1024);
+  const RowShape q = row_shape(s.D * (int64_t)s.esz / 16, true);
+  const int64_t nt = lnorm_threads(q.gs), groups = nt / q.gs;
+  return std::min<int64_t>((s.T + groups - 1) / groups, nt == 256 ? 768 : nt == 512 ? 512 : 256);
 }
 
 // f(integral_constant GS, integral_constant CH) of a row shape
-template <typename E, typename F>
+template <typename E, bool BWD, typename F>
 static void with_row_shape(const RowShape& q, F&& f) {
   auto go = [&](auto GSc, auto CHc) {
     if (q.gs == GSc.value && q.ch == CHc.value) f(GSc, CHc);
@@ -306,9 +317,14 @@ static void with_row_shape(const RowShape& q, F&& f) {
   go(std::integral_constant<int, 32>{}, c1);
   go(std::integral_constant<int, 64>{}, c1);
   go(std::integral_constant<int, 64>{}, c2);
-  go(std::integral_constant<int, 64>{}, c4);
   go(std::integral_constant<int, 256>{}, c2);
-  go(std::integral_constant<int, 256>{}, c4);
+  if constexpr (BWD) {
+    go(std::integral_constant<int, 256>{}, c1);
+    go(std::integral_constant<int, 512>{}, c2);
+  } else {
+    go(std::integral_constant<int, 64>{}, c4);
+    go(std::integral_constant<int, 256>{}, c4);
+  }
   go(std::integral_constant<int, 512>{}, c4);
   if constexpr (sizeof(E) == 4) go(std::integral_constant<int, 1024>{}, c4);
 }
@@ -316,9 +332,9 @@ static void with_row_shape(const RowShape& q, F&& f) {
 template <typename E>
 static void layer_norm_fwd(const Shape& s, const void* x, const void* res, const void* gamma, const void* beta, void* sum,
                            void* y, float* stats, hipStream_t st) {
-  const RowShape q = row_shape(s.D / Vec<E>::N);
+  const RowShape q = row_shape(s.D / Vec<E>::N, false);
   auto c = [](const void* p) { return reinterpret_cast<const E*>(p); };
-  with_row_shape<E>(q, [&](auto GSc, auto CHc) {
+  with_row_shape<E, false>(q, [&](auto GSc, auto CHc) {
     constexpr int GS = decltype(GSc)::value, CH = decltype(CHc)::value, NT = lnorm_threads(GS), G = NT / GS;
     const int64_t blocks = std::min<int64_t>((s.T + G - 1) / G, 256 * (2048 / NT));
     auto kern = res ? layer_norm_fwd_kernel<E, GS, CH, true> : layer_norm_fwd_kernel<E, GS, CH, false>;
@@ -330,17 +346,17 @@ static void layer_norm_fwd(const Shape& s, const void* x, const void* res, const
 template <typename E>
 static void layer_norm_bwd(const Shape& s, const void* sum, const float* stats, const void* gamma, const void* dy,
                            const void* dres, void* dx, void* dgamma, void* dbeta, float* part, hipStream_t st) {
-  const RowShape q = row_shape(s.D / Vec<E>::N);
+  const RowShape q = row_shape(s.D / Vec<E>::N, true);
   const int nb = (int)lnorm_bwd_blocks(s);
   auto c = [](const void* p) { return reinterpret_cast<const E*>(p); };
   if (nb > 0)
-    with_row_shape<E>(q, [&](auto GSc, auto CHc) {
+    with_row_shape<E, true>(q, [&](auto GSc, auto CHc) {
       constexpr int GS = decltype(GSc)::value, CH = decltype(CHc)::value, NT = lnorm_threads(GS);
       auto kern = dres ? layer_norm_bwd_kernel<E, GS, CH, true> : layer_norm_bwd_kernel<E, GS, CH, false>;
       DMOE_LAUNCH_NAMED("layer_norm_bwd_kernel", kern, dim3(nb), dim3(NT), 0, st, c(sum), stats, c(gamma), c(dy),
                         c(dres), reinterpret_cast<E*>(dx), part, (int)s.T, (int)s.D);
     });
-  DMOE_LAUNCH_NAMED("layer_norm_reduce_kernel", layer_norm_reduce_kernel<E>, dim3((unsigned)(2 * s.D / LR_C)), dim3(LR_NT),
+  DMOE_LAUNCH_NAMED("layer_norm_reduce_kernel", layer_norm_reduce_kernel<E>, dim3((unsigned)(2 * s.D / (4 * LR_C))), dim3(LR_NT),
                     0, st, part, nb, (int)s.D, reinterpret_cast<E*>(dgamma), reinterpret_cast<E*>(dbeta));
 }
 

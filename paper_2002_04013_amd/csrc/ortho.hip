@@ -676,7 +676,8 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
 
 constexpr int GR_COLS = 128;              // columns of X in LDS
 constexpr int GR_SLICES = 32;             // most partial sums of A_0
-constexpr int GR_NT = 256;
+constexpr int GR_NT = 512;
+constexpr int GS_NT = 1024;               // of the steps: a wave to a tile at r = 64
 
 // Columns c0 .. c0 + GR_COLS - 1 of X = U (not normalised), fp32 in LDS, zeros past r and c.
 template <typename E, bool FIRST>
@@ -707,7 +708,7 @@ __device__ __forceinline__ void gram_slice(const UpdateArgs& a, int64_t base, in
   __syncthreads();
 }
 
-// part[e][block] [R16][R16] = U U^T over the block's columns, fp64; a wave keeps up to four of
+// part[e][block] [R16][R16] = U U^T over the block's columns, fp64; a wave keeps up to two of
 // its 16 x 16 tiles.
 template <typename E>
 __global__ void __launch_bounds__(GR_NT) gram_kernel(UpdateArgs a, double* part) {
@@ -716,13 +717,13 @@ __global__ void __launch_bounds__(GR_NT) gram_kernel(UpdateArgs a, double* part)
   if (!on(a, e)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nt = (min(a.m, a.n) + 15) / 16, R16 = nt * 16;
   const int g = lane >> 4, c = max(a.m, a.n), pieces = (c + GR_COLS - 1) / GR_COLS;
-  f64x4_t acc[4] = {};
+  f64x4_t acc[2] = {};
   for (int s = blockIdx.x; s < pieces; s += gridDim.x) {
     __syncthreads();
     gram_slice<E, true>(a, (int64_t)e * a.m * a.n, s * GR_COLS, x);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = wave + 4 * i;
+    for (int i = 0; i < 2; ++i) {
+      const int t = wave + GR_NT / 64 * i;
       if (t >= nt * nt) continue;
       const float* xi = x[t / nt * 16 + (lane & 15)];
       const float* xj = x[t % nt * 16 + (lane & 15)];
@@ -733,8 +734,8 @@ __global__ void __launch_bounds__(GR_NT) gram_kernel(UpdateArgs a, double* part)
   }
   double* o = part + ((int64_t)e * gridDim.x + blockIdx.x) * R16 * R16;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int t = wave + 4 * i;
+  for (int i = 0; i < 2; ++i) {
+    const int t = wave + GR_NT / 64 * i;
     if (t < nt * nt)
 #pragma unroll
       for (int v = 0; v < 4; ++v) o[(t / nt * 16 + 4 * v + (lane >> 4)) * R16 + t % nt * 16 + (lane & 15)] = acc[i][v];
@@ -747,7 +748,7 @@ __device__ __forceinline__ void mat_mul(double* C, const double* A, const double
                                         double s2, double s3) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   __syncthreads();
-  for (int t = wave; t < nt * nt; t += GR_NT / 64) {
+  for (int t = wave; t < nt * nt; t += GS_NT / 64) {
     const int ti = t / nt * 16, tj = t % nt * 16;
     f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
     const double* ai = A + (ti + (lane & 15)) * GL + (lane >> 4);
@@ -764,7 +765,7 @@ __device__ __forceinline__ void mat_mul(double* C, const double* A, const double
 }
 
 // P[e] [R16][R16]: the polynomial of all steps, times 1 / (|U| + eps).  A block to a matrix.
-__global__ void __launch_bounds__(GR_NT) gram_steps_kernel(UpdateArgs a, const double* part, int slices, int steps, double* P) {
+__global__ void __launch_bounds__(GS_NT) gram_steps_kernel(UpdateArgs a, const double* part, int slices, int steps, double* P) {
   extern __shared__ __align__(16) char smem[];
   double* A = reinterpret_cast<double*>(smem);
   double* Q = A + GRAM_R * GL;
@@ -774,7 +775,7 @@ __global__ void __launch_bounds__(GR_NT) gram_steps_kernel(UpdateArgs a, const d
   const int e = blockIdx.x;
   if (!on(a, e)) return;
   const int nt = (min(a.m, a.n) + 15) / 16, R16 = nt * 16;
-  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) {
+  for (int q = threadIdx.x; q < R16 * R16; q += GS_NT) {
     const int i = q / R16, j = q % R16;
     double s = 0.0;
     const double* src = part + (int64_t)e * slices * R16 * R16 + q;
@@ -792,7 +793,7 @@ __global__ void __launch_bounds__(GR_NT) gram_steps_kernel(UpdateArgs a, const d
   }
   __syncthreads();
   const double f = inv;
-  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) A[q / R16 * GL + q % R16] *= f * f;
+  for (int q = threadIdx.x; q < R16 * R16; q += GS_NT) A[q / R16 * GL + q % R16] *= f * f;
   for (int k = 0; k < steps; ++k) {
     mat_mul(Q, A, A, nt, NS_C, A, NS_B, NS_A);
     mat_mul(Z, Q, Pl, nt, 1.0, nullptr, 0.0, 0.0);
@@ -803,37 +804,38 @@ __global__ void __launch_bounds__(GR_NT) gram_steps_kernel(UpdateArgs a, const d
     }
   }
   __syncthreads();
-  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) P[(int64_t)e * R16 * R16 + q] = Pl[q / R16 * GL + q % R16] * f;
+  for (int q = threadIdx.x; q < R16 * R16; q += GS_NT) P[(int64_t)e * R16 * R16 + q] = Pl[q / R16 * GL + q % R16] * f;
 }
 
-// O (or the parameters) = P U, slice by slice.
+// O (or the parameters) = P U, slice by slice; a wave to 16 columns.
 template <typename E>
 __global__ void __launch_bounds__(GR_NT) gram_apply_kernel(UpdateArgs a, const double* P) {
   __shared__ float x[GRAM_R][GR_COLS + 4];
+  __shared__ double Ps[GRAM_R * GL];
+  static_assert(GR_COLS / 16 == GR_NT / 64, "a wave to 16 columns");
   const int e = blockIdx.y;
   if (!on(a, e)) return;
   const int64_t base = (int64_t)e * a.m * a.n;
   const int c0 = blockIdx.x * GR_COLS;
   const bool turn = a.m > a.n;
   const int r = turn ? a.n : a.m, c = turn ? a.m : a.n;
-  gram_slice<E, false>(a, base, c0, x);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nt = (r + 15) / 16, R16 = nt * 16;
-  const double* Pe = P + (int64_t)e * R16 * R16;
-  constexpr int CT = GR_COLS / 16;
-  for (int t = wave; t < nt * CT; t += GR_NT / 64) {
-    const int ti = t / CT * 16, tj = t % CT * 16;
+  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) Ps[q / R16 * GL + q % R16] = P[(int64_t)e * R16 * R16 + q];
+  gram_slice<E, false>(a, base, c0, x);
+  const int l16 = lane & 15, g = lane >> 4, tj = wave * 16;
+  for (int ti = 0; ti < R16; ti += 16) {
     f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
     for (int k0 = 0; k0 < R16; k0 += 16)
 #pragma unroll
       for (int k1 = 0; k1 < 16; k1 += 4) {
-        const int k = k0 + k1 + (lane >> 4);
-        const double pk = Pe[(ti + (lane & 15)) * R16 + k], xk = (double)x[k][tj + (lane & 15)];
+        const int k = k0 + k1 + g;
+        const double pk = Ps[(ti + l16) * GL + k], xk = (double)x[k][tj + l16];
         acc = __builtin_amdgcn_mfma_f64_16x16x4f64(turn ? xk : pk, turn ? pk : xk, acc, 0, 0, 0);
       }
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       // 16 lanes along a row of the result
-      const int i = ti + (turn ? lane & 15 : 4 * v + (lane >> 4)), j = c0 + tj + (turn ? 4 * v + (lane >> 4) : lane & 15);
+      const int i = ti + (turn ? l16 : 4 * v + g), j = c0 + tj + (turn ? 4 * v + g : l16);
       if (i < r && j < c) store_at<E>(a, base + (turn ? (int64_t)j * a.n + i : (int64_t)i * a.n + j), (float)acc[v]);
     }
   }
@@ -960,7 +962,7 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     constexpr int lds = 4 * GRAM_R * GL * (int)sizeof(double);
     (void)hipFuncSetAttribute((const void*)gram_steps_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     (void)hipGetLastError();
-    DMOE_LAUNCH(gram_steps_kernel, dim3((unsigned)q.B), dim3(GR_NT), lds, st, u, part, o.slices, q.steps, P);
+    DMOE_LAUNCH(gram_steps_kernel, dim3((unsigned)q.B), dim3(GS_NT), lds, st, u, part, o.slices, q.steps, P);
     DMOE_LAUNCH_NAMED("gram_apply_kernel", gram_apply_kernel<E>, grid, dim3(GR_NT), 0, st, u, P);
     return;
   }
