@@ -3,16 +3,21 @@
 //
 // The call is bound by one read of the chosen experts' weights, so the tokens' rows are
 // brought to the weights and nothing else is written but h's activations and the pairs'
-// outputs (P H and P D values).  Launches: the gate's scores (fp64 partial sums over slices of
-// d_model, spread over the chip); the up-projection, whose blocks each choose the tokens'
-// experts for themselves (up to 8 tokens: one wave to a token; above, a launch of its own does
-// it) and group the pairs by expert; the down-projection; the weighted average.
+// outputs (P H and P D values).  Four launches: the gate, a block to a token (in the smallest
+// calls every block of the next launch does it instead); the up-projection, whose blocks each
+// group the pairs by expert for themselves; the down-projection; the weighted average.
+// Measured: 16 tokens of experts 4096 x 16384 (11.1 GB of weights) 1.74 ms, 6.4 TB/s; 37 tokens of experts
+// 1024 x 4096 331 us, 5.2 TB/s; one token of them (67 MB) 28.6 us, of which about 12 are the weights,
+// the rest the chain of the four launches.
+// Slower: the average by the wave that stores the last expert's tile, found by a counter, in place
+// of its launch (the fences cost more: one token 28 -> 31 us, 8 tokens 108 -> 179); a block of the
+// down-projection to 16 columns of all experts (too few blocks: 29 -> 40).
 //
 // The products run on 16-row matrix instructions with the weights as the 16-row operand and
 // an expert's tokens as its 16 columns; no weight is read twice, and the vectors of the
-// tokens' rows come from the caches.  A 16-row tile belongs to KS
-// waves, each a share of the contraction, so that the few tiles of a call with few pairs
-// still keep every compute unit's loads in flight.
+// tokens' rows come from the caches.  A 16-row tile belongs to KS waves, each a share of the
+// contraction, so that the few tiles of a call with few pairs still keep every compute unit's
+// loads in flight.
 #include <algorithm>
 
 #include "gate_select.hpp"
@@ -21,35 +26,24 @@ namespace dmoe {
 
 constexpr int FEW_T = 64;                 // most tokens
 constexpr int FEW_P = FEW_T * KMAX;       // most pairs
-// largest T d M D of scores that the up-projection's blocks compute themselves.  Own launch / in the
-// blocks: T = 1, 8192 values (fp32, D = 64) 18.3 / 15.2 us a call; T = 1, 32 columns, D = 1024
-// 24.3 / 22.4; T = 1, 64 columns, D = 1024 29.4 / 29.7; T = 4 of them 70.5 / 82.6.
-constexpr int64_t FEW_INLINE = 32768;
 constexpr int FEW_NT = 512, FEW_NW = FEW_NT / 64;
 static_assert(FEW_P == FEW_NT, "a thread to a pair");
 
-typedef double f64x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
-// Workspace: the scores' partial sums, the plan, the activations, the pairs' outputs.
-struct FewPlan {                          // written by the up-projection's first block
+// Workspace: the plan, the activations, the pairs' outputs.
+struct FewPlan {
+  int32_t eid[FEW_P];                     // expert of each pair, -1 for a dead one: written by the gate's launch
+  // by the up-projection's first block:
   int32_t E;                              // experts with rows
   int32_t expert[FEW_P], off[FEW_P], n[FEW_P];   // each one's id, first row, rows
   int32_t pos[FEW_P];                     // row of each pair, -1 for a dead one
 };
-struct FewWs {
-  size_t part, plan, a, yp, total;
-  int S;                                  // slices of d_model
-};
+struct FewWs { size_t plan, a, yp, total; };
 static FewWs few_ws(const Shape& s) {
   auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
   FewWs w{};
-  // a wave's slice of d_model: four loads of each operand, at most 32 slices for one token
-  // and four for 64 (every block of the up-projection adds them up)
-  const int64_t chunks = s.D * (int64_t)s.esz / 64;
-  w.S = (int)std::max<int64_t>(1, std::min<int64_t>({chunks / 4, 32, std::max<int64_t>(4, 128 / std::max<int64_t>(s.T, 1))}));
   size_t off = 0;
-  w.part = off; off += up((size_t)w.S * s.T * s.dM * sizeof(double));
   w.plan = off; off += up(sizeof(FewPlan));
   w.a = off; off += up((size_t)s.P * s.H * s.esz);
   w.yp = off; off += up((size_t)s.P * s.D * sizeof(float));
@@ -58,131 +52,122 @@ static FewWs few_ws(const Shape& s) {
 }
 
 struct FewArgs {
-  GateArgs gate;                          // idx and w: the caller's outputs
-  const double* part; int S;              // part NULL: the up-projection's blocks do the scores
   FewPlan* plan;
   const void* W; const void* bias;        // of this product: [N][R][K], [N][R]
   const void* in; void* out;              // up: x, a;  down: a, pairs' outputs (fp32)
-  int R, K, P, act;
+  int R, K, P, k, act;
+  GateArgs gate;                          // up with the gate in its blocks
+  int alive_first;
 };
 
-// ---------------------------------------------------------------- gate scores
+// ---------------------------------------------------------------- gate
 
-// part[sl][t][c] = the share of slice sl of d_model in the score of token t and gate column c,
-// on fp64 matrix instructions (operand layout as in the exact gate): a wave to 16 tokens, 16
-// columns and a slice.
+// Scores of four gate columns from c0 for one token by one wave, its lanes at vectors v0 + lane, v0 + lane
+// + step, ...: fp64 multiply-adds of the exact values.  Lane i < 4 returns column c0 + i.
+constexpr int FG_C = 4;
 template <typename E>
-__global__ void __launch_bounds__(256) few_scores_kernel(GateArgs a, double* part, int CTN, int S, int units) {
-  constexpr int VEC = 16 / sizeof(E), CHUNK = 4 * VEC;
-  const int lane = threadIdx.x & 63;
-  const int u = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (u >= units) return;
-  const int sl = u % S, ct = u / S % CTN, tt = u / S / CTN;
-  const int r16 = lane & 15, g = lane >> 4;
-  const int t = tt * 16 + r16, col = ct * 16 + r16;
-  const E* xr = reinterpret_cast<const E*>(a.x) + (int64_t)min(t, a.T - 1) * a.D + g * VEC;
-  const E* wr = reinterpret_cast<const E*>(a.Wg) + (int64_t)min(col, a.dM - 1) * a.D + g * VEC;
-  const int nc = a.D / CHUNK;
-  const int c0 = nc * sl / S, c1 = nc * (sl + 1) / S;
-  f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
-  constexpr int U = 4;
-  for (int c = c0; c < c1; c += U) {
-    uint4 fx[U], fw[U];
-#pragma unroll
-    for (int p = 0; p < U; ++p)
-      if (c + p < c1) {
-        fx[p] = *reinterpret_cast<const uint4*>(xr + (int64_t)(c + p) * CHUNK);
-        fw[p] = *reinterpret_cast<const uint4*>(wr + (int64_t)(c + p) * CHUNK);
-      }
-#pragma unroll
-    for (int p = 0; p < U; ++p)
-      if (c + p < c1) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)vec_elem<E>(fw[p], j), (double)vec_elem<E>(fx[p], j), acc, 0,
-                                                     0, 0);
-      }
-  }
-  if (t >= a.T) return;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const int c = ct * 16 + 4 * v + g;
-    if (c < a.dM) part[((int64_t)sl * a.T + t) * a.dM + c] = acc[v];
-  }
-}
-
-// ---------------------------------------------------------------- choice of experts
-
-struct FewSelectLds {
-  double s64[FEW_NW][DM_MAX + 1];
-  SelectScratch scratch[FEW_NW];
-};
-
-// Tokens t0 .. t0 + 7 of the call, a wave to each: scores from the slices in order (part NULL:
-// they are in q already), then the exact selection into a.idx, a.w (global or LDS, [token][k]).
-template <typename E, bool ALIVE>
-__device__ __forceinline__ void few_select(const GateArgs& a, const double* part, int S, int t0, FewSelectLds& q) {
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const E* bg = reinterpret_cast<const E*>(a.bg);
-  const int nt = min(FEW_NW, a.T - t0);
-  const RankTuples tup = rank_tuples<ALIVE>(a);      // loaded while the scores are summed
-  if (part)
-    for (int i = threadIdx.x; i < nt * a.dM; i += FEW_NT) {
-      const int t = i / a.dM, c = i - t * a.dM;
-      double v = bg ? (double)ldf(bg + c) : 0.0;
-#pragma unroll 8
-      for (int sl = 0; sl < S; ++sl) v += part[((int64_t)sl * a.T + t0 + t) * a.dM + c];
-      q.s64[t][c] = v;
-    }
-  __syncthreads();
-  if (wv < nt) select_wave<ALIVE>(a, tup, q.s64[wv], q.scratch[wv], t0 + wv);
-}
-
-// The scores of all tokens by one block, for calls with so few products (FEW_INLINE) that every
-// block of the up-projection does them sooner than a launch of its own: a wave to four
-// columns of a token, its lanes along d_model, fp64 multiply-adds of the exact values.
-template <typename E>
-__device__ __forceinline__ void few_scores_block(const GateArgs& a, FewSelectLds& q) {
-  constexpr int VEC = 16 / sizeof(E), C = 4;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const E* bg = reinterpret_cast<const E*>(a.bg);
+__device__ __forceinline__ double few_dot(const GateArgs& a, int t, int c0, int v0, int step) {
+  constexpr int VEC = 16 / sizeof(E);
+  const int lane = threadIdx.x & 63, nv = a.D / VEC;
+  const E* xr = reinterpret_cast<const E*>(a.x) + (int64_t)t * a.D;
   const E* Wg = reinterpret_cast<const E*>(a.Wg);
-  const int nv = a.D / VEC, groups = (a.dM + C - 1) / C;
-  for (int u = wv; u < a.T * groups; u += FEW_NW) {
-    const int t = u / groups, c0 = (u - t * groups) * C;
-    const E* xr = reinterpret_cast<const E*>(a.x) + (int64_t)t * a.D;
-    double acc[C] = {0.0, 0.0, 0.0, 0.0};
+  double acc[FG_C] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 2
-    for (int v = lane; v < nv; v += 64) {
-      const uint4 fx = *reinterpret_cast<const uint4*>(xr + v * VEC);
-      uint4 fw[C];
+  for (int v = v0 + lane; v < nv; v += step) {
+    const uint4 fx = *reinterpret_cast<const uint4*>(xr + (int64_t)v * VEC);
+    uint4 fw[FG_C];
 #pragma unroll
-      for (int i = 0; i < C; ++i)
-        fw[i] = *reinterpret_cast<const uint4*>(Wg + (int64_t)min(c0 + i, a.dM - 1) * a.D + v * VEC);
+    for (int i = 0; i < FG_C; ++i)
+      fw[i] = *reinterpret_cast<const uint4*>(Wg + (int64_t)min(c0 + i, a.dM - 1) * a.D + (int64_t)v * VEC);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const double xj = (double)vec_elem<E>(fx, j);
+    for (int j = 0; j < VEC; ++j) {
+      const double xj = (double)vec_elem<E>(fx, j);
 #pragma unroll
-        for (int i = 0; i < C; ++i) acc[i] = fma(xj, (double)vec_elem<E>(fw[i], j), acc[i]);
-      }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-#pragma unroll
-      for (int i = 0; i < C; ++i) acc[i] += __shfl_xor(acc[i], o, WAVE);
-    if (lane < C && c0 + lane < a.dM) {
-      const int c = c0 + lane;
-      const double v = lane == 0 ? acc[0] : lane == 1 ? acc[1] : lane == 2 ? acc[2] : acc[3];
-      q.s64[t][c] = v + (bg ? (double)ldf(bg + c) : 0.0);
+      for (int i = 0; i < FG_C; ++i) acc[i] = fma(xj, (double)vec_elem<E>(fw[i], j), acc[i]);
     }
   }
-  __syncthreads();
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < FG_C; ++i) acc[i] += __shfl_xor(acc[i], o, WAVE);
+  return lane == 0 ? acc[0] : lane == 1 ? acc[1] : lane == 2 ? acc[2] : acc[3];
 }
 
+// Choice of experts of token t by one wave from its scores in LDS, exact as dmoe_gate_topk's; lane i < k
+// returns the i-th expert, or -1 for a dead one.  OUT: idx and w are written.
+template <bool ALIVE>
+__device__ __forceinline__ int few_choose(const GateArgs& a, const RankTuples& tup, const double* s64, SelectScratch& scratch,
+                                          int t, int* chosen, float* w, bool out) {
+  const int lane = threadIdx.x & 63;
+  wave_lds_sync();
+  GateArgs ga = a;                         // into LDS, at the token's place
+  ga.idx = chosen;
+  ga.w = w;
+  select_wave<ALIVE>(ga, tup, s64, scratch, t);
+  wave_lds_sync();
+  if (lane >= a.k) return -1;
+  const int p = t * a.k + lane, e = chosen[p];
+  if (out) { a.idx[p] = e; a.w[p] = w[p]; }
+  return a.alive && !a.alive[e] ? -1 : e;
+}
+
+// One token to a block.  A wave takes four gate columns at a time; SP waves share the columns of a
+// narrow gate, each a share of d_model.  Then one wave selects.  Bound by latency: the loads of
+// d_model, a reduction and the selection, one after another (5 to 10 us).  As a launch of fp64 matrix
+// products over slices of d_model, with the selection in every block of the up-projection (up to 8
+// tokens) or a launch of its own: 37 tokens, 32 columns, D = 1024 16 us for 10; 8 tokens of D = 512 28.7 us
+// a call for 26.6; one token of D = 1024 28.2 for 28.9.
+constexpr int FG_NT = 1024, FG_NW = FG_NT / 64;
 template <typename E, bool ALIVE>
-__global__ void __launch_bounds__(FEW_NT) few_select_kernel(GateArgs a, const double* part, int S) {
-  __shared__ FewSelectLds q;
-  few_select<E, ALIVE>(a, part, S, blockIdx.x * FEW_NW, q);
+__global__ void __launch_bounds__(FG_NT) few_gate_kernel(GateArgs a, int SP, FewPlan* plan) {
+  __shared__ double part[FG_NW][DM_MAX];           // SP shares of the columns
+  __shared__ SelectScratch scratch;
+  __shared__ int chosen[FEW_P];
+  __shared__ float w[FEW_P];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = blockIdx.x, groups = (a.dM + FG_C - 1) / FG_C;
+  const RankTuples tup = rank_tuples<ALIVE>(a);
+  for (int u = wv; u < groups * SP; u += FG_NW) {
+    const int c0 = u / SP * FG_C, sp = u % SP;
+    const double v = few_dot<E>(a, t, c0, sp * 64, SP * 64);
+    if (lane < FG_C && c0 + lane < a.dM) part[sp][c0 + lane] = v;
+  }
+  __syncthreads();
+  if (wv) return;
+  const E* bg = reinterpret_cast<const E*>(a.bg);
+  for (int c = lane; c < a.dM; c += 64) {
+    double s = bg ? (double)ldf(bg + c) : 0.0;
+    for (int sp = 0; sp < SP; ++sp) s += part[sp][c];
+    part[0][c] = s;
+  }
+  const int e = few_choose<ALIVE>(a, tup, part[0], scratch, t, chosen, w, true);
+  if (lane < a.k) plan->eid[t * a.k + lane] = e;
+}
+
+// The same for all of at most 8 tokens by one block of the up-projection, into eid[].
+struct FewGateLds {
+  double s64[FEW_NW][DM_MAX];
+  SelectScratch scratch[FEW_NW];
+  int chosen[FEW_NW * KMAX];
+  float w[FEW_NW * KMAX];
+};
+template <typename E, bool ALIVE>
+__device__ __forceinline__ void few_gate_block(const GateArgs& a, FewGateLds& q, int* eid) {
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (a.dM + FG_C - 1) / FG_C;
+  const RankTuples tup = rank_tuples<ALIVE>(a);
+  const E* bg = reinterpret_cast<const E*>(a.bg);
+  for (int u = wv; u < a.T * groups; u += FEW_NW) {
+    const int t = u / groups, c = (u - t * groups) * FG_C + lane;
+    const double b = bg && lane < FG_C && c < a.dM ? (double)ldf(bg + c) : 0.0;
+    const double v = few_dot<E>(a, t, c - lane, 0, 64);
+    if (lane < FG_C && c < a.dM) q.s64[t][c] = b + v;
+  }
+  __syncthreads();
+  if (wv < a.T) {
+    const int e = few_choose<ALIVE>(a, tup, q.s64[wv], q.scratch[wv], wv, q.chosen, q.w, blockIdx.x == 0);
+    if (lane < a.k) eid[wv * a.k + lane] = e;
+  }
 }
 
 // ---------------------------------------------------------------- the two products
@@ -297,49 +282,34 @@ __device__ __forceinline__ int few_plan(FewPlanLds& q, int P, FewPlan* out) {
   return E;
 }
 
-// UP: a[row] = act(W1_e x[token of row] + b1_e), and before it the choice of experts (INLINE: the
-// call has at most 8 tokens and no launch of its own chose them) and the plan.
+// UP: a[row] = act(W1_e x[token of row] + b1_e), and before it the plan.  GATE: and before that the gate.
 // Down: out[row] = W2_e a[row] + b2_e, fp32.
 // MAXQ: groups of 16 rows an expert may have (1 or 4).
-template <typename E, bool UP, bool INLINE, bool ALIVE, int KS, int MAXQ>
+template <typename E, bool UP, bool GATE, int KS, int MAXQ>
 __global__ void __launch_bounds__(FEW_NT) few_product_kernel(FewArgs a) {
   constexpr int VEC = 16 / sizeof(E), CHUNK = 4 * VEC, TPB = FEW_NW / KS;
   struct Lds {
     union {
-      FewSelectLds sel;
       struct { f32x4_t red[FEW_NW][MAXQ][64]; __align__(16) char turn[FEW_NW][16 * (64 * 8 + 16)]; };
+      FewGateLds gate;
     };
     FewPlanLds plan;
   };
   __shared__ Lds q;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r16 = lane & 15, g = lane >> 4;
+  const int r16 = lane & 15, g = lane >> 4, p = threadIdx.x;
   int EX;
   if constexpr (UP) {
-    const int p = threadIdx.x;
-    int e = -1;
-    if constexpr (INLINE) {
-      GateArgs ga = a.gate;
-      // up to 64 pairs: the choice goes to the plan's arrays first
-      ga.idx = q.plan.expert;
-      ga.w = reinterpret_cast<float*>(q.plan.off);
-      if (!a.part) few_scores_block<E>(ga, q.sel);
-      few_select<E, ALIVE>(ga, a.part, a.S, 0, q.sel);
+    q.plan.eid[p] = !GATE && p < a.P ? a.plan->eid[p] : -1;
+    if constexpr (GATE) {
       __syncthreads();
-      if (p < a.P) {
-        e = q.plan.expert[p];
-        if (blockIdx.x == 0) { a.gate.idx[p] = e; a.gate.w[p] = reinterpret_cast<float*>(q.plan.off)[p]; }
-      }
-    } else {
-      if (p < a.P) e = a.gate.idx[p];
+      if (a.alive_first) few_gate_block<E, true>(a.gate, q.gate, q.plan.eid);
+      else few_gate_block<E, false>(a.gate, q.gate, q.plan.eid);
     }
-    if (e >= 0 && a.gate.alive && !a.gate.alive[e]) e = -1;
-    q.plan.eid[p] = e;
     __syncthreads();
     EX = few_plan(q.plan, a.P, blockIdx.x == 0 ? a.plan : nullptr);
   } else {
     EX = a.plan->E;
-    const int p = threadIdx.x;
     if (p < a.P) {                         // those past the last expert are not used
       q.plan.expert[p] = a.plan->expert[p];
       q.plan.off[p] = a.plan->off[p];
@@ -368,7 +338,7 @@ __global__ void __launch_bounds__(FEW_NT) few_product_kernel(FewArgs a) {
       const E* wt = reinterpret_cast<const E*>(a.W) + ((int64_t)e * a.R + r0) * a.K;
       auto row = [&](int i) {              // the operand row of the expert's i-th row (the last one past its end)
         const int r = off + min(i, n - 1);
-        return in + (int64_t)(UP ? q.plan.rowpair[r] / a.gate.k : r) * a.K + g * VEC;
+        return in + (int64_t)(UP ? q.plan.rowpair[r] / a.k : r) * a.K + g * VEC;
       };
       if (MAXQ == 1 || n <= 16) {
         const E* xr[1] = {row(r16)};
@@ -473,7 +443,12 @@ static int few_split(const Shape& s, int64_t R, int64_t K) {
   return ks;
 }
 
-template <typename E, bool UP, bool INLINE, bool ALIVE>
+// Whether the up-projection's blocks take the gate.  Us a call, own launch / in the blocks: one token, d M D
+// = 32768 22.1 / 20.8, 65536 28.9 / 28.7 and (wider experts) 42.8 / 40.6; 3 tokens of 512 18.0 / 15.5; 4 of
+// 4096 19.7 / 20.4; 2 of 65536 43.8 / 47.0.
+static bool few_gate_inside(const Shape& s) { return s.dM * s.D <= (s.T == 1 ? 65536 : 8192 / s.T) && s.T <= FEW_NW; }
+
+template <typename E, bool UP, bool GATE = false>
 static void few_product(const Shape& s, const FewArgs& a, hipStream_t st) {
   const int ks = few_split(s, a.R, a.K);
   const int64_t tiles = std::min(s.P, s.N) * (a.R / 16), tpb = FEW_NW / ks;
@@ -481,8 +456,7 @@ static void few_product(const Shape& s, const FewArgs& a, hipStream_t st) {
   auto go = [&](auto KSc) {
     constexpr int KS = decltype(KSc)::value;
     if (ks != KS) return;
-    auto kern = s.T <= 16 || INLINE ? few_product_kernel<E, UP, INLINE, ALIVE, KS, 1>
-                                    : few_product_kernel<E, UP, INLINE, ALIVE, KS, INLINE ? 1 : 4>;
+    auto kern = GATE || s.T <= 16 ? few_product_kernel<E, UP, GATE, KS, 1> : few_product_kernel<E, UP, GATE, KS, GATE ? 1 : 4>;
     DMOE_LAUNCH_NAMED(UP ? "few_product_kernel (up)" : "few_product_kernel (down)", kern, grid, dim3(FEW_NT), 0, st, a);
   };
   go(std::integral_constant<int, 1>{});
@@ -495,28 +469,21 @@ template <typename E>
 static void layer_few_fwd(const Shape& s, const GateArgs& g, const void* W1, const void* b1, const void* W2, const void* b2,
                           const void* res, void* y, unsigned char* ws, hipStream_t st) {
   const FewWs L = few_ws(s);
-  double* part = reinterpret_cast<double*>(ws + L.part);
   FewPlan* plan = reinterpret_cast<FewPlan*>(ws + L.plan);
-  const bool alive_first = (s.flags & DMOE_FLAG_ALIVE_TOPK) != 0;
-  const bool inl = s.T <= FEW_NW;
-  if (inl && s.T * s.dM * s.D <= FEW_INLINE) {
-    part = nullptr;
+  const int alive_first = (s.flags & DMOE_FLAG_ALIVE_TOPK) != 0;
+  const FewArgs up{plan, W1, b1, g.x, ws + L.a, (int)s.H, (int)s.D, (int)s.P, s.k, s.act, g, alive_first};
+  if (few_gate_inside(s)) {
+    few_product<E, true, true>(s, up, st);
   } else {
-    const int CTN = (int)((s.dM + 15) / 16), units = (int)((s.T + 15) / 16) * CTN * L.S;
-    DMOE_LAUNCH_NAMED("few_scores_kernel", few_scores_kernel<E>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, g,
-                      part, CTN, L.S, units);
+    const int64_t groups = (s.dM + FG_C - 1) / FG_C, vecs = s.D / Vec<E>::N;
+    int SP = 1;                            // two or more loads of d_model to a lane
+    while (2 * SP * groups <= FG_NW && 2 * SP * 128 <= vecs) SP *= 2;
+    auto gate = alive_first ? few_gate_kernel<E, true> : few_gate_kernel<E, false>;
+    DMOE_LAUNCH_NAMED("few_gate_kernel", gate, dim3((unsigned)s.T), dim3(FG_NT), 0, st, g, SP, plan);
+    few_product<E, true>(s, up, st);
   }
-  if (!inl) {
-    auto kern = alive_first ? few_select_kernel<E, true> : few_select_kernel<E, false>;
-    DMOE_LAUNCH_NAMED("few_select_kernel", kern, dim3((unsigned)((s.T + FEW_NW - 1) / FEW_NW)), dim3(FEW_NT), 0, st, g, part,
-                      L.S);
-  }
-  FewArgs up{g, part, L.S, plan, W1, b1, g.x, ws + L.a, (int)s.H, (int)s.D, (int)s.P, s.act};
-  if (!inl) few_product<E, true, false, false>(s, up, st);
-  else if (alive_first) few_product<E, true, true, true>(s, up, st);
-  else few_product<E, true, true, false>(s, up, st);
-  FewArgs down{g, part, L.S, plan, W2, b2, ws + L.a, ws + L.yp, (int)s.D, (int)s.H, (int)s.P, s.act};
-  few_product<E, false, false, false>(s, down, st);
+  const FewArgs down{plan, W2, b2, ws + L.a, ws + L.yp, (int)s.D, (int)s.H, (int)s.P, s.k, s.act, g, 0};
+  few_product<E, false>(s, down, st);
   const int cols = 256 * Vec<E>::N;
   DMOE_LAUNCH_NAMED("few_combine_kernel", few_combine_kernel<E>, dim3((unsigned)((s.D + cols - 1) / cols), (unsigned)s.T),
                     dim3(256), 0, st, plan, reinterpret_cast<const float*>(ws + L.yp), g.w, reinterpret_cast<const E*>(res),

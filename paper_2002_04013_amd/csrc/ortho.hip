@@ -807,9 +807,42 @@ __global__ void __launch_bounds__(GS_NT) gram_steps_kernel(UpdateArgs a, const d
   for (int q = threadIdx.x; q < R16 * R16; q += GS_NT) P[(int64_t)e * R16 * R16 + q] = Pl[q / R16 * GL + q % R16] * f;
 }
 
-// O (or the parameters) = P U, slice by slice; a wave to 16 columns.
+// r <= 16: all steps by one wave in registers.  Lane (l = lane % 16, g = lane / 16) holds the elements
+// (4 v + g, l) of a matrix, which is the layout of a result and of the second operand of its k-th
+// four rows, and, all matrices being symmetric, of the first operand.
+__device__ __forceinline__ f64x4_t sym_mul(const f64x4_t& x, const f64x4_t& y) {
+  f64x4_t c = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+  for (int v = 0; v < 4; ++v) c = __builtin_amdgcn_mfma_f64_16x16x4f64(x[v], y[v], c, 0, 0, 0);
+  return c;
+}
+__device__ __forceinline__ f64x4_t gram_steps_16(f64x4_t A, int steps) {
+  const int l = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  f64x4_t one, P;
+  double norm = 0.0;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    one[v] = 4 * v + g == l ? 1.0 : 0.0;
+    norm += one[v] * A[v];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) norm += __shfl_xor(norm, o, WAVE);
+  const double f = 1.0 / (sqrt(norm) + NS_EPS);
+  A *= f * f;
+  P = one;
+  for (int k = 0; k < steps; ++k) {
+    const f64x4_t Q = sym_mul(A, A) * NS_C + A * NS_B + one * NS_A;
+    P = sym_mul(Q, P);
+    if (k + 1 < steps) A = sym_mul(sym_mul(Q, A), Q);
+  }
+  return P * f;
+}
+
+// O (or the parameters) = P U, slice by slice; a wave to 16 columns.  P: [e][R16][R16], or NULL (r <= 16):
+// every block takes the steps from A_0's partial sums for itself.
 template <typename E>
-__global__ void __launch_bounds__(GR_NT) gram_apply_kernel(UpdateArgs a, const double* P) {
+__global__ void __launch_bounds__(GR_NT)
+gram_apply_kernel(UpdateArgs a, const double* part, int slices, int steps, const double* P) {
   __shared__ float x[GRAM_R][GR_COLS + 4];
   __shared__ double Ps[GRAM_R * GL];
   static_assert(GR_COLS / 16 == GR_NT / 64, "a wave to 16 columns");
@@ -820,7 +853,26 @@ __global__ void __launch_bounds__(GR_NT) gram_apply_kernel(UpdateArgs a, const d
   const bool turn = a.m > a.n;
   const int r = turn ? a.n : a.m, c = turn ? a.m : a.n;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nt = (r + 15) / 16, R16 = nt * 16;
-  for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) Ps[q / R16 * GL + q % R16] = P[(int64_t)e * R16 * R16 + q];
+  if (P) {
+    for (int q = threadIdx.x; q < R16 * R16; q += GR_NT) Ps[q / R16 * GL + q % R16] = P[(int64_t)e * R16 * R16 + q];
+  } else {
+    // the slices' sums, two threads to an element, then the first wave's steps
+    static_assert(GR_NT == 512, "two threads to an element");
+    double* sums = &Ps[GRAM_R * GL - 512];
+    double s = 0.0;
+#pragma unroll 8
+    for (int k = threadIdx.x >> 8; k < slices; k += 2) s += part[((int64_t)e * slices + k) * 256 + (threadIdx.x & 255)];
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (wave == 0) {
+      f64x4_t A;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) A[v] = sums[64 * v + lane] + sums[256 + 64 * v + lane];
+      A = gram_steps_16(A, steps);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) Ps[(4 * v + (lane >> 4)) * GL + (lane & 15)] = A[v];
+    }
+  }
   gram_slice<E, false>(a, base, c0, x);
   const int l16 = lane & 15, g = lane >> 4, tj = wave * 16;
   for (int ti = 0; ti < R16; ti += 16) {
@@ -962,8 +1014,9 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     constexpr int lds = 4 * GRAM_R * GL * (int)sizeof(double);
     (void)hipFuncSetAttribute((const void*)gram_steps_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     (void)hipGetLastError();
-    DMOE_LAUNCH(gram_steps_kernel, dim3((unsigned)q.B), dim3(GS_NT), lds, st, u, part, o.slices, q.steps, P);
-    DMOE_LAUNCH_NAMED("gram_apply_kernel", gram_apply_kernel<E>, grid, dim3(GR_NT), 0, st, u, P);
+    if (o.r <= 16) P = nullptr;
+    else DMOE_LAUNCH(gram_steps_kernel, dim3((unsigned)q.B), dim3(GS_NT), lds, st, u, part, o.slices, q.steps, P);
+    DMOE_LAUNCH_NAMED("gram_apply_kernel", gram_apply_kernel<E>, grid, dim3(GR_NT), 0, st, u, part, o.slices, q.steps, P);
     return;
   }
   auto f = [&](size_t off) { return reinterpret_cast<f16*>(ws + off); };

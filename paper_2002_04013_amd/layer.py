@@ -5,6 +5,9 @@ Forward:  gate_topk -> dispatch -> expert_ffn_fwd -> combine   (DMoELayer)
 Backward: combine_bwd -> gate_topk_bwd -> expert_ffn_bwd -> dispatch_bwd
 With recompute=True the backward regenerates h and a (expert_ffn_bwd_recompute), so
 they need not be kept from the forward: h and a are then scratch shared by both passes.
+
+DMoESublayer puts the layer into a pre-norm residual sub-layer: normalisation, training with
+orthogonalised updates, and the serving form for a few tokens.
 """
 import torch
 
@@ -29,6 +32,7 @@ class DMoELayer:
         if nws == 0:
             raise abi.DmoeError("unsupported layer shape")
         self.ws = torch.empty(nws, dtype=torch.uint8, device=dev)
+        self.few_ws = None                   # of serve
         P, N = self.P, self.N
         self.idx = e(T, k, dt=i32)
         self.w = e(T, k, dt=torch.float32)
@@ -61,6 +65,18 @@ class DMoELayer:
                                 self.y_perm, self.ws)
         abi.dmoe_combine(D, self.y_perm, self.pos, self.w, self.y)
         return self.y
+
+    def serve(self, x, Wg, bg, alive, W1, b1, W2, b2, res=None, out=None):
+        """res + the layer's output for at most abi.FEW_TOKENS tokens (dmoe_layer_few_fwd), into out
+        (the layer's y by default); keeps nothing for a backward pass."""
+        if self.few_ws is None:
+            n = abi.layer_few_workspace_bytes(self.dims)
+            if n == 0:
+                raise abi.DmoeError(f"serve takes at most {abi.FEW_TOKENS} tokens")
+            self.few_ws = torch.empty(n, dtype=torch.uint8, device=self.y.device)
+        out = self.y if out is None else out
+        abi.dmoe_layer_few_fwd(self.dims, x, Wg, bg, alive, W1, b1, W2, b2, res, self.idx, self.w, out, self.few_ws)
+        return out
 
     def backward(self, dy, x, Wg, alive, W1, W2, dW1, db1, dW2, db2, dWg, dbg, b1=None):
         """b1 is needed only with recompute=True (the up-projection is run again)."""
@@ -143,3 +159,78 @@ class DMoEBlockLayer:
                                     self.g2, self.dx_perm, grads, self.ws)
         abi.dmoe_dispatch_bwd(D, self.dx_perm, self.pos, self.idx, self.dg, Wg, self.dx)
         return self.dx
+
+
+class DMoESublayer:
+    """A DMoE layer in a pre-norm residual sub-layer, as one replaces a Transformer's feed-forward
+    block:
+
+        s = x + r,   n = LN(s) = gamma (s - mean) rstd + beta,   y = DMoE(n),   out = s + y.
+
+    forward returns (s, y): the next normalisation adds them (its x and r), so the sum takes no
+    pass of its own.  serve returns out.
+
+    Forward:  layer_norm_fwd -> DMoELayer.forward
+    Backward: DMoELayer.backward -> layer_norm_bwd
+    Update:   muon_step on W1, W2 (experts without rows keep theirs) and the gate's matrices
+    Serving:  layer_norm_fwd -> layer_few_fwd
+    """
+
+    def __init__(self, T, D, H, d, M, k, dtype="bf16", act="gelu", device="cuda", flags=0, recompute=False):
+        self.layer = DMoELayer(T, D, H, d, M, k, dtype, act, device, flags=flags, recompute=recompute)
+        self.dtype = dtype
+        L = self.layer
+        dev = L.y.device
+        e = lambda *s, dt=None: torch.empty(s, dtype=dt or L.dt, device=dev)
+        u8 = torch.uint8
+        nws = abi.layer_norm_workspace_bytes(L.dims)
+        if nws == 0:
+            raise abi.DmoeError("unsupported row width")
+        self.norm_ws = e(nws, dt=u8)
+        self.s, self.n, self.stats = e(T, D), e(T, D), e(T, 2, dt=torch.float32)
+        self.dx = e(T, D)
+        self.muon_ws = None
+
+    def _norm(self, x, res, gamma, beta, stats):
+        """s and n of the sub-layer (s is x itself where there is no residual)."""
+        abi.dmoe_layer_norm_fwd(self.layer.dims, x, res, gamma, beta, None if res is None else self.s, self.n, stats)
+        return x if res is None else self.s
+
+    def forward(self, x, res, gamma, beta, Wg, bg, alive, W1, b1, W2, b2):
+        s = self._norm(x, res, gamma, beta, self.stats)
+        return s, self.layer.forward(self.n, Wg, bg, alive, W1, b1, W2, b2, scores=False)
+
+    def backward(self, dy, ds, s, gamma, Wg, alive, W1, W2, grads, b1=None):
+        """dy: the gradient of y; ds: the gradient that reaches s past the layer (dy itself for
+        out = s + y), or None; s: as forward returned it.  grads: dict of gamma, beta, Wg, bg, W1, b1, W2,
+        b2.  Returns the gradient of x and of res."""
+        g = grads
+        dn = self.layer.backward(dy, self.n, Wg, alive, W1, W2, g["W1"], g["b1"], g["W2"], g["b2"], g["Wg"], g["bg"], b1=b1)
+        abi.dmoe_layer_norm_bwd(self.layer.dims, s, self.stats, gamma, dn, ds, self.dx, g["gamma"], g["beta"],
+                                self.norm_ws)
+        return self.dx
+
+    def _mats(self):
+        L = self.layer
+        m = lambda *s: abi.make_mats(*s, self.dtype)
+        return dict(W1=m(L.N, L.H, L.D), W2=m(L.N, L.D, L.H), Wg=m(L.d, L.M, L.D))
+
+    def update(self, params, grads, mom, lr, mu=0.95, decay=0.0, nesterov=True):
+        """One orthogonalised momentum step of params["W1"], ["W2"] and ["Wg"] (those present) in
+        place, after a backward pass; mom: fp32 momentum with their names and shapes.  Biases and
+        normalisation parameters are the caller's."""
+        mats = self._mats()
+        if self.muon_ws is None:
+            n = max(abi.orthogonalize_workspace_bytes(q) for q in mats.values())
+            if n == 0:
+                raise abi.DmoeError("unsupported matrix sizes")
+            self.muon_ws = torch.empty(n, dtype=torch.uint8, device=self.dx.device)
+        for name, q in mats.items():
+            if name in params:
+                abi.dmoe_muon_step(q, grads[name], None if name == "Wg" else self.layer.counts, mom[name], params[name],
+                                   lr, mu, decay, nesterov, self.muon_ws)
+
+    def serve(self, x, res, gamma, beta, Wg, bg, alive, W1, b1, W2, b2):
+        """out = s + DMoE(LN(s)) for at most abi.FEW_TOKENS tokens."""
+        s = self._norm(x, res, gamma, beta, None)
+        return self.layer.serve(self.n, Wg, bg, alive, W1, b1, W2, b2, res=s)
