@@ -325,12 +325,29 @@ struct NsArgs {
   int full, S;                            // tiles past `full` are split into S slices of the contraction:
   float* part;                            // their sums
   float down;                             // result (its scale included) over accumulator
+  // NS_SYM, pair > 0: `pair` matrices of this product, then as many of another with the same left operand
+  int pair;
+  const f16 *Bh2, *Bl2;
+  f16 *Ch2, *Cl2;
+  float down2;
   int e0;                                 // first matrix
   UpdateArgs u;
 };
 
 // blocks are dealt to the eight XCDs in turn: each takes a contiguous run of tiles (count a multiple of 8)
 __device__ __forceinline__ int xcd_run(int b, int count) { return (b & 7) * (count >> 3) + (b >> 3); }
+
+// Matrix g of a launch: of the second product past the first's, with that product's arguments.
+template <int P>
+__device__ __forceinline__ int take_pair(NsArgs& p, int g) {
+  if constexpr (P == NS_SYM) {
+    if (p.pair && g >= p.pair) {
+      p.Bh = p.Bh2; p.Bl = p.Bl2; p.Ch = p.Ch2; p.Cl = p.Cl2; p.down = p.down2;
+      return g - p.pair;
+    }
+  }
+  return g;
+}
 
 // Tile t of a matrix: row ti, column tj.  Symmetric results: the lower triangle, row by row.
 template <int P>
@@ -378,7 +395,7 @@ ns_product_kernel(NsArgs p) {
   const int S = sliced ? p.S : 1, s = sliced ? u % S : 0;
   const int L = sliced ? p.full + u / S : xcd_run((int)blockIdx.x, p.full);
   if (L >= p.total) return;
-  const int t = L % p.tiles, g = L / p.tiles;
+  const int t = L % p.tiles, g = take_pair<P>(p, L / p.tiles);
   if (!on(p.u, p.e0 + g)) return;
   int ti, tj;
   tile_at<P>(p, t, ti, tj);
@@ -619,7 +636,7 @@ ns_product_kernel(NsArgs p) {
 template <typename E, int P, int T>
 __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
   constexpr int WN = T / 64, TM = T / 64, TN = 2, PIECES = 2 * WN * TM * TN;
-  const int piece = blockIdx.x % PIECES, u = blockIdx.x / PIECES, L = p.full + u, g = L / p.tiles, t = L % p.tiles;
+  const int piece = blockIdx.x % PIECES, u = blockIdx.x / PIECES, L = p.full + u, t = L % p.tiles, g = take_pair<P>(p, L / p.tiles);
   if (!on(p.u, p.e0 + g)) return;
   int ti, tj;
   tile_at<P>(p, t, ti, tj);
@@ -964,16 +981,16 @@ static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
   for (size_t* p : {&o->xh[0], &o->xl[0], &o->xh[1], &o->xl[1]}) { *p = off; off += up(g * o->Rp * o->Cp * 2); }
   // Steps to one pass over X (see the top): estimated, the fewest passes against none saved.
   const NsTiling gram = ns_tiling(o->group, true, o->Rp, o->Rp, o->Cp), sym = ns_tiling(o->group, true, o->Rp, o->Rp, o->Rp),
-                 apply = ns_tiling(o->group, false, o->Rp, o->Cp, o->Rp);
+                 pair = ns_tiling(2 * o->group, true, o->Rp, o->Rp, o->Rp), apply = ns_tiling(o->group, false, o->Rp, o->Cp, o->Rp);
   const int most = std::min<int>(q->steps, q->dtype == DMOE_BF16 ? NS_MERGE_BF16 : NS_MERGE_F32);
-  const double one = gram.us + sym.us + apply.us, many = gram.us + (4 * most - 3) * sym.us + apply.us;
+  const double one = gram.us + sym.us + apply.us, many = gram.us + sym.us + (most - 1) * (2 * sym.us + (most > 2 ? pair.us : 2 * sym.us)) + apply.us;
   o->merge = many < most * one ? most : 1;
   for (int i = 0; i < (o->merge > 1 ? 6 : 3); ++i)
     for (size_t* p : {&o->sh[i], &o->sl[i]}) { *p = off; off += up(g * o->Rp * o->Rp * 2); }
   size_t sums = 0;
   for (int64_t k : {(int64_t)o->group, q->B % o->group})          // whole groups and the last one
     for (const NsTiling& t : {ns_tiling(k, true, o->Rp, o->Rp, o->Cp), ns_tiling(k, true, o->Rp, o->Rp, o->Rp),
-                              ns_tiling(k, false, o->Rp, o->Cp, o->Rp)})
+                              ns_tiling(2 * k, true, o->Rp, o->Rp, o->Rp), ns_tiling(k, false, o->Rp, o->Cp, o->Rp)})
       if (t.S > 1) sums = std::max(sums, (size_t)(t.total - t.full) * t.S * t.T * t.T * sizeof(float));
   o->sums = off; off += up(sums);
   o->total = off;
@@ -1049,27 +1066,29 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
       int P = -1;                          // the steps' product so far, held at SPLIT / 4^(steps - 1)
       float up = 1.f;
       for (int i = 0; i < merge; ++i) {
-        const int Q = Q0 + (i & 1);
+        const int Q = Q0 + (i & 1), next = i == 0 ? Q : P0 + (i & 1);
         left(A); right(A); to(Q);
         p.down = 1.f / SPLIT;
         ns_product<float, NS_POLY>(p, g, o.Rp, o.Rp, st);
-        if (i == 0) {
-          P = Q;
-        } else {
-          left(Q); right(P);
-          P = P0 + (i & 1);
-          to(P);
-          p.down = 0.25f / SPLIT;
-          ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
-          up *= 4.f;
-        }
-        if (i + 1 < merge) {               // A of the next step
-          p.down = 1.f / SPLIT;
-          left(Q); right(A); to(AQ);
-          ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
+        left(Q);
+        if (i > 0) up *= 4.f;
+        if (i + 1 < merge) {               // A of the next step, A Q together with the product
+          if (i > 0) {
+            p.pair = g;
+            p.Bh2 = f(o.sh[P]); p.Bl2 = f(o.sl[P]); p.Ch2 = f(o.sh[next]); p.Cl2 = f(o.sl[next]);
+            p.down2 = 0.25f / SPLIT;
+          }
+          to(AQ);
+          ns_product<float, NS_SYM>(p, i > 0 ? 2 * g : g, o.Rp, o.Rp, st);
+          p.pair = 0;
           left(AQ); right(Q); to(A);
           ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
+        } else if (i > 0) {
+          right(P); to(next);
+          p.down = 0.25f / SPLIT;
+          ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
         }
+        P = next;
       }
       k += merge;
       left(P);
