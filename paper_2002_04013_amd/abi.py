@@ -134,7 +134,7 @@ def _ptr(t):
         raise DmoeError("libdmoe takes device tensors only")
     if not t.is_contiguous():
         raise DmoeError("libdmoe takes contiguous tensors only")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()          # the arguments' and fields' type is c_void_p (an object of it: 0.1 us each)
 
 
 # The current stream's handle without the Stream object around it (2.8 us a call on the

@@ -101,7 +101,7 @@ __device__ __forceinline__ void store_row(const UpdateArgs& a, int64_t at, float
 
 // ---------------------------------------------------------------- r > 64: norm and operands
 
-constexpr int NB_MAX = 64;                // blocks to a matrix of the norm
+constexpr int NB_MAX = 512;               // most blocks to a matrix of the norm
 
 // part[e][block] = sum of U^2 over the block's share, in fp64 (squares of fp32 values overflow
 // fp32); advances the momentum.  WIDE: 16 bytes of G to a thread (m n a multiple of them), else
@@ -175,7 +175,10 @@ ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* hi, f1
   const int g = blockIdx.z, e = e0 + g;
   if (!on(a, e)) return;
   if (threadIdx.x < 64) {
-    double s = (int)threadIdx.x < nb ? part[(int64_t)g * NB_MAX + threadIdx.x] : 0.0;
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < NB_MAX / 64; ++i)
+      if ((int)threadIdx.x + 64 * i < nb) s += part[(int64_t)g * NB_MAX + threadIdx.x + 64 * i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
     if (threadIdx.x == 0) inv = (double)SPLIT / (sqrt(s) + NS_EPS);
@@ -975,7 +978,7 @@ static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
   // matrices at a time: enough 128 x 128 tiles for 16 rounds of the compute units, two to each
   const int64_t tiles = o->Rp / 128 * (o->Cp / 128);
   o->group = (int)std::max<int64_t>(1, std::min<int64_t>(q->B, (8192 + tiles - 1) / tiles));
-  o->nb = (int)std::max<int64_t>(1, std::min<int64_t>(NB_MAX, q->m * q->n / 4096));
+  o->nb = (int)std::max<int64_t>(1, std::min<int64_t>({NB_MAX, (2048 + o->group - 1) / o->group, q->m * q->n / 4096}));
   const size_t g = (size_t)o->group;
   o->part = off; off += up(g * NB_MAX * sizeof(double));
   for (size_t* p : {&o->xh[0], &o->xl[0], &o->xh[1], &o->xl[1]}) { *p = off; off += up(g * o->Rp * o->Cp * 2); }

@@ -4,7 +4,8 @@ Error bounds.  The step maps singular values by p(s) = a s + b s^3 + c s^5; on [
 differences of p are at most 4.25, so an error E of X becomes at most 4.25 |E|_F (Frobenius) after one step.  What a step
 adds itself (r > 64): operands held to 2^-22 of a value (two fp16 values of 11 bits; the product of the two low parts is
 left out, 2^-22 of a product) and fp32 sums of 3 K products, of errors 6 sqrt(3 K) 2^-24 with all but 1e-8 probability (sums of
-independent roundings), against products of absolute values.  r <= 64: fp64 throughout; what is left is the
+independent roundings), against products of absolute values.  Steps that share a pass over X are asked for the bound of
+single steps too.  r <= 64: fp64 throughout; what is left is the
 rounding of the result."""
 import math
 
