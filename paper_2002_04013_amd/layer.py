@@ -9,6 +9,8 @@ they need not be kept from the forward: h and a are then scratch shared by both 
 DMoESublayer puts the layer into a pre-norm residual sub-layer: normalisation, training with
 orthogonalised updates, and the serving form for a few tokens.
 """
+from types import SimpleNamespace
+
 import torch
 
 from . import abi
@@ -32,7 +34,7 @@ class DMoELayer:
         if nws == 0:
             raise abi.DmoeError("unsupported layer shape")
         self.ws = torch.empty(nws, dtype=torch.uint8, device=dev)
-        self.few_ws = None                   # of serve
+        self.few = None                      # of serve
         P, N = self.P, self.N
         self.idx = e(T, k, dt=i32)
         self.w = e(T, k, dt=torch.float32)
@@ -68,15 +70,23 @@ class DMoELayer:
 
     def serve(self, x, Wg, bg, alive, W1, b1, W2, b2, res=None, out=None):
         """res + the layer's output for at most abi.FEW_TOKENS tokens (dmoe_layer_few_fwd), into out
-        (the layer's y by default); keeps nothing for a backward pass."""
-        if self.few_ws is None:
+        (few.y by default).  Keeps nothing for a backward pass and leaves alone what a forward has
+        kept; the choice is in few.idx and few.w."""
+        F = self._few()
+        out = F.y if out is None else out
+        abi.dmoe_layer_few_fwd(self.dims, x, Wg, bg, alive, W1, b1, W2, b2, res, F.idx, F.w, out, F.ws)
+        return out
+
+    def _few(self):
+        """serve's buffers, made by its first call."""
+        if self.few is None:
             n = abi.layer_few_workspace_bytes(self.dims)
             if n == 0:
                 raise abi.DmoeError(f"serve takes at most {abi.FEW_TOKENS} tokens")
-            self.few_ws = torch.empty(n, dtype=torch.uint8, device=self.y.device)
-        out = self.y if out is None else out
-        abi.dmoe_layer_few_fwd(self.dims, x, Wg, bg, alive, W1, b1, W2, b2, res, self.idx, self.w, out, self.few_ws)
-        return out
+            e = torch.empty_like
+            self.few = SimpleNamespace(ws=torch.empty(n, dtype=torch.uint8, device=self.y.device), idx=e(self.idx),
+                                       w=e(self.w), y=e(self.y), s=e(self.y), n=e(self.y))
+        return self.few
 
     def backward(self, dy, x, Wg, alive, W1, W2, dW1, db1, dW2, db2, dWg, dbg, b1=None):
         """b1 is needed only with recompute=True (the up-projection is run again)."""
@@ -191,13 +201,13 @@ class DMoESublayer:
         self.dx = e(T, D)
         self.muon_ws = None
 
-    def _norm(self, x, res, gamma, beta, stats):
+    def _norm(self, x, res, gamma, beta, s, n, stats):
         """s and n of the sub-layer (s is x itself where there is no residual)."""
-        abi.dmoe_layer_norm_fwd(self.layer.dims, x, res, gamma, beta, None if res is None else self.s, self.n, stats)
-        return x if res is None else self.s
+        abi.dmoe_layer_norm_fwd(self.layer.dims, x, res, gamma, beta, None if res is None else s, n, stats)
+        return x if res is None else s
 
     def forward(self, x, res, gamma, beta, Wg, bg, alive, W1, b1, W2, b2):
-        s = self._norm(x, res, gamma, beta, self.stats)
+        s = self._norm(x, res, gamma, beta, self.s, self.n, self.stats)
         return s, self.layer.forward(self.n, Wg, bg, alive, W1, b1, W2, b2, scores=False)
 
     def backward(self, dy, ds, s, gamma, Wg, alive, W1, W2, grads, b1=None):
@@ -231,6 +241,7 @@ class DMoESublayer:
                                    lr, mu, decay, nesterov, self.muon_ws)
 
     def serve(self, x, res, gamma, beta, Wg, bg, alive, W1, b1, W2, b2):
-        """out = s + DMoE(LN(s)) for at most abi.FEW_TOKENS tokens."""
-        s = self._norm(x, res, gamma, beta, None)
-        return self.layer.serve(self.n, Wg, bg, alive, W1, b1, W2, b2, res=s)
+        """out = s + DMoE(LN(s)) for at most abi.FEW_TOKENS tokens; leaves alone what a forward has kept."""
+        F = self.layer._few()
+        s = self._norm(x, res, gamma, beta, F.s, F.n, None)
+        return self.layer.serve(F.n, Wg, bg, alive, W1, b1, W2, b2, res=s)

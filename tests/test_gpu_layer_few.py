@@ -120,6 +120,29 @@ def test_dead_experts(T, p_alive, alive_topk, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("alive_topk", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [4, 30])
+def test_rows_that_are_not_finite(T, dtype, alive_topk):
+    """A row of NaN, or with infinities of both signs, goes to valid experts and spoils no other row; an expert of NaN
+    that answers no one spoils none."""
+    D, H, d, M, k = 128, 192, 2, 4, 2
+    q = _inputs(T, D, H, d, M, k, dtype, 4321, 0.7)
+    ridx, rw, ry, bound = _reference(q, T, d, M, k, dtype, "gelu", alive_topk)
+    q["x"][1] = float("nan")
+    q["x"][2, ::2], q["x"][2, 1::2] = float("inf"), -float("inf")
+    dead = int((q["alive"] == 0).nonzero()[0])
+    for n in ("W1", "b1", "W2", "b2"):
+        q[n][dead] = float("nan")
+    idx, w, y = _run(q, T, D, H, d, M, k, dtype, "gelu", alive_topk)
+    assert ((idx >= 0) & (idx < M ** d)).all()
+    ok = [t for t in range(T) if t not in (1, 2)]
+    assert np.array_equal(idx[ok], ridx[ok])
+    assert (np.abs(w - rw)[ok] <= (16 + 64) * U * rw[ok]).all()
+    assert (np.abs(y - ry)[ok] <= bound[ok]).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("kw", [dict(bg=False), dict(alive=False), dict(res=False), dict(bg=False, alive=False, res=False)])
 def test_left_out_arguments(kw):
     _check(f"without {sorted(kw)}", 5, 128, 128, 2, 3, 2, "bf16", "gelu", 0.7, **kw)

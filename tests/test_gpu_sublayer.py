@@ -114,7 +114,7 @@ def test_training_step_of_two_sublayers(recompute):
     o1 = serve[1].serve(o0, None, *P(1))
     s0, y0 = sub[0].forward(x.cuda(), None, *P(0))
     s1, y1 = sub[1].forward(y0, s0, *P(1))
-    assert torch.equal(serve[1].layer.idx, sub[1].layer.idx[:few])
+    assert torch.equal(serve[1].layer.few.idx, sub[1].layer.idx[:few])
     _near(o1, (s1 + y1)[:few].double().cpu(), tol, "served")
 
 
@@ -135,7 +135,7 @@ def test_serving_bf16(T):
                     dev["W2"], dev["b2"])
     r = {n: v.double() for n, v in p.items()}
     s = (x.double() + res.double()).bfloat16().double()
-    _, y = _reference(s, None, r, alive, sub.layer.idx.long().cpu(), d, M, "gelu")
+    _, y = _reference(s, None, r, alive, sub.layer.few.idx.long().cpu(), d, M, "gelu")
     say(f"[sublayer] {T}")
     _near(out, s + y, 6 * 2.0 ** -8, "out")
 
@@ -184,3 +184,26 @@ def test_serve_takes_few_tokens_only():
     x = torch.zeros(65, 64, device="cuda")
     with pytest.raises(abi.DmoeError):
         sub.serve(x, None, dev["gamma"], dev["beta"], dev["Wg"], dev["bg"], None, dev["W1"], dev["b1"], dev["W2"], dev["b2"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("recompute", [False, True])
+def test_serving_between_forward_and_backward(recompute):
+    """A served batch between a forward and its backward changes nothing of the step: bit for bit."""
+    T, D, H, d, M, k = 24, 128, 192, 2, 3, 2
+    dev = {n: v.cuda() for n, v in _params(D, H, d, M, "bf16", 5).items()}
+    x, r, dout, x2, r2 = (torch.randn(T, D, device="cuda").bfloat16() for _ in range(5))
+    P = [dev[n] for n in ("gamma", "beta", "Wg", "bg")] + [None] + [dev[n] for n in ("W1", "b1", "W2", "b2")]
+    want = None
+    for between in (False, True):
+        sub = DMoESublayer(T, D, H, d, M, k, "bf16", recompute=recompute)
+        grads = {n: torch.zeros_like(v) for n, v in dev.items()}
+        s, y = sub.forward(x, r, *P)
+        served = sub.serve(x2, r2, *P).clone() if between else None
+        dx = sub.backward(dout, dout, s, dev["gamma"], dev["Wg"], None, dev["W1"], dev["W2"], grads, b1=dev["b1"])
+        got = [s, y, dx] + [grads[n] for n in dev]
+        if between:
+            assert all(torch.equal(p, q) for p, q in zip(got, want))
+            fresh = DMoESublayer(T, D, H, d, M, k, "bf16")
+            assert torch.equal(served, fresh.serve(x2, r2, *P))
+        want = [q.clone() for q in got]
