@@ -165,11 +165,17 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
   lo = (f16)(v - (float)hi);
 }
 
-// X (hi and lo planes [Rp][Cp]) = U / (|U| + eps), padded with zeros; a block to a 64 x 64 piece,
+// An operand [rows][ld / 2] is held as [rows][ld / 64][hi, lo][32]: a row's 32 values of one LDS stage are
+// 128 contiguous bytes, a whole line of the caches (with a plane each for hi and lo, of which a stage
+// takes half a line at a time: OLDNEW).
+__device__ __forceinline__ int64_t at_op(int64_t row, int col, int64_t ld) { return row * ld + (col >> 5) * 64 + (col & 31); }
+constexpr int LO = 32;                    // from a value's hi to its lo
+
+// X = U / (|U| + eps), an operand [Rp][Cp] padded with zeros; a block to a 64 x 64 piece,
 // turned through LDS where m > n.  WIDE: 16 bytes of G to a thread (n a multiple of them).
 template <typename E, bool WIDE>
 __global__ void __launch_bounds__(256)
-ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* hi, f16* lo, int Rp, int Cp, int64_t plane) {
+ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* X, int Rp, int Cp) {
   __shared__ float tile[64][65];
   __shared__ double inv;
   const int g = blockIdx.z, e = e0 + g;
@@ -241,9 +247,9 @@ ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* hi, f1
       split((float)((double)(turn ? tile[x + k][y] : tile[y][x + k]) * f), vh, vl);
       h[k] = vh; l[k] = vl;
     }
-    const int64_t at = g * plane + (int64_t)(y0 + y) * Cp + x0 + x;
-    *reinterpret_cast<f16x8_t*>(hi + at) = h;
-    *reinterpret_cast<f16x8_t*>(lo + at) = l;
+    f16* o = X + (int64_t)g * 2 * Rp * Cp + at_op(y0 + y, x0 + x, 2 * Cp);
+    *reinterpret_cast<f16x8_t*>(o) = h;
+    *reinterpret_cast<f16x8_t*>(o + LO) = l;
   }
 }
 
@@ -260,44 +266,45 @@ __device__ __forceinline__ void g2l(const f16* base, uint32_t off_bytes, char* l
 
 constexpr int NS_BK = 32;                 // contraction of one LDS stage
 
-// Tile of R rows contiguous along the contraction, [R][32]: 16-byte chunk c of row i at position
-// c ^ ((i / 4) % 4), so that 16 rows read at one chunk fall on 16 bank groups.
+// Tile of R rows contiguous along the contraction, [R][hi, lo][32]: 16-byte chunk c of row i at
+// position c ^ ((i / 2) % 8), so that 16 rows read at one chunk fall on 16 bank groups.
 template <int R, int NW>
 struct RowTile {
-  static constexpr int BYTES = R * 64, PER_WAVE = R / 16 / NW;
-  static_assert(R % (16 * NW) == 0, "whole instructions to a wave");
+  static constexpr int BYTES = R * 128, PER_WAVE = R / 8 / NW;
+  static_assert(R % (8 * NW) == 0, "whole instructions to a wave");
   __device__ __forceinline__ static void load(const f16* base, int ld, char* lds, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) {
-      const int q = wave + i * NW, row = q * 16 + lane / 4, c = (lane & 3) ^ ((row >> 2) & 3);
+      const int q = wave + i * NW, row = q * 8 + lane / 8, c = (lane & 7) ^ ((row >> 1) & 7);
       g2l(base, ((uint32_t)row * (uint32_t)ld + (uint32_t)(c * 8)) * 2u, lds + q * 1024);
     }
   }
-  // operand of rows i0 .. i0 + 31 and contraction kk .. kk + 15 (kk = 0 or 16)
-  __device__ __forceinline__ static f16x8_t frag(const char* lds, int i0, int kk, int lane) {
-    const int row = i0 + (lane & 31), c = (kk / 8 + (lane >> 5)) ^ ((row >> 2) & 3);
-    return *reinterpret_cast<const f16x8_t*>(lds + row * 64 + c * 16);
+  // operand of rows i0 .. i0 + 31 and contraction kk .. kk + 15 (kk = 0 or 16); part: 0 hi, 1 lo
+  __device__ __forceinline__ static f16x8_t frag(const char* lds, int i0, int kk, int part, int lane) {
+    const int row = i0 + (lane & 31), c = (4 * part + kk / 8 + (lane >> 5)) ^ ((row >> 1) & 7);
+    return *reinterpret_cast<const f16x8_t*>(lds + row * 128 + c * 16);
   }
 };
 
-// Tile of R columns, [32][R], contiguous across the contraction: chunk c of row k at position
-// c ^ (4 (k % 4)); operands come from transposing reads.
+// Tile of R columns, [32][R / 32][hi, lo][32], contiguous across the contraction: chunk c of row k at
+// position c ^ (4 (k % 4)); operands come from transposing reads.
 template <int R, int NW>
 struct ColTile {
-  static constexpr int BYTES = R * 64, RPI = 512 / R, PER_WAVE = R / 16 / NW;
+  static constexpr int BYTES = R * 128, RPI = 256 / R, PER_WAVE = R / 8 / NW;
   __device__ __forceinline__ static void load(const f16* base, int ld, char* lds, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) {
-      const int q = wave + i * NW, k = q * RPI + lane / (R / 8), c = (lane % (R / 8)) ^ (4 * (k & 3));
+      const int q = wave + i * NW, k = q * RPI + lane / (R / 4), c = (lane % (R / 4)) ^ (4 * (k & 3));
       g2l(base, ((uint32_t)k * (uint32_t)ld + (uint32_t)(c * 8)) * 2u, lds + q * 1024);
     }
   }
-  __device__ __forceinline__ static f16x8_t frag(const char* lds, int c0, int kk, int lane) {
+  __device__ __forceinline__ static f16x8_t frag(const char* lds, int c0, int kk, int part, int lane) {
     const int g = lane >> 4, i = lane & 15;
     const int col = c0 + 16 * (g & 1) + 4 * (i & 3), k = kk + 8 * (g >> 1) + (i >> 2);
-    const char* at = lds + k * (2 * R) + (((col >> 3) ^ (4 * (k & 3))) << 4) + (col & 7) * 2;   // k and k + 4: same position
+    const int c = (col >> 5) * 8 + part * 4 + ((col & 31) >> 3);
+    const char* at = lds + k * (4 * R) + ((c ^ (4 * (k & 3))) << 4) + (col & 7) * 2;   // k and k + 4: same position
     const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
-    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(at + 4 * 2 * R));
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(at + 4 * 4 * R));
     const s16x8_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(f16x8_t, v);
   }
@@ -320,9 +327,9 @@ enum NsProduct {
 };
 
 struct NsArgs {
-  const f16 *Ah, *Al, *Bh, *Bl;           // operands (hi, lo planes), matrix by matrix
-  f16 *Ch, *Cl;                           // result planes
-  int lda, ldb, ldc, K;                   // multiples of 32
+  const f16 *A, *B;                       // operands, matrix by matrix
+  f16* C;                                 // result
+  int lda, ldb, ldc, K;                   // lengths of their rows (twice as many values), multiples of 64; contraction
   int64_t sa, sb, sc;                     // strides of the matrices
   int TI, tiles, total;                   // rows of tiles, tiles of a matrix and of all
   int full, S;                            // tiles past `full` are split into S slices of the contraction:
@@ -330,8 +337,8 @@ struct NsArgs {
   float down;                             // result (its scale included) over accumulator
   // NS_SYM, pair > 0: `pair` matrices of this product, then as many of another with the same left operand
   int pair;
-  const f16 *Bh2, *Bl2;
-  f16 *Ch2, *Cl2;
+  const f16* B2;
+  f16* C2;
   float down2;
   int e0;                                 // first matrix
   UpdateArgs u;
@@ -345,7 +352,7 @@ template <int P>
 __device__ __forceinline__ int take_pair(NsArgs& p, int g) {
   if constexpr (P == NS_SYM) {
     if (p.pair && g >= p.pair) {
-      p.Bh = p.Bh2; p.Bl = p.Bl2; p.Ch = p.Ch2; p.Cl = p.Cl2; p.down = p.down2;
+      p.B = p.B2; p.C = p.C2; p.down = p.down2;
       return g - p.pair;
     }
   }
@@ -374,11 +381,13 @@ __device__ __forceinline__ float ns_value(float acc, float down, float ah, float
 }
 
 // One T x T tile to a block (8 waves of 128 x 64 for T = 256, 4 of 64 x 64 for 128): two LDS stages of
-// 32, the next one loading while the current one is multiplied.  A CU's LDS moves 128 bytes a
-// cycle: 2048 cycles of reads and loads to 3072 of products for T = 256, as many as of products for 128,
-// two blocks to a unit.  MFMAs are busy 70% of the time at T = 256, at 1.6 GHz (the clock the power
-// limit leaves): 1273 TFLOP/s of fp16 products at r = 4096, c = 16384, where a library product of
-// 8192 x 8192 runs at 1470.  Four stages for T = 128 (a block to a unit): 1 to 10% slower.
+// 32, the next one loading while the current one is multiplied.  At the 64 bytes a cycle that a CU's LDS
+// was seen to move, a stage's operand reads take 1.3 times the cycles of its products for T = 256 and
+// twice for 128, where two blocks share a unit.  With all units busy the power limit bounds it as much:
+// MFMAs are busy 70% of the time at T = 256, at 1.6 GHz: 1273 TFLOP/s of fp16 products at r = 4096,
+// c = 16384, where a library product of 8192 x 8192 runs at 1470.  Operands straight from memory to
+// registers, kept in their order, no LDS: 5% faster there, 5 to 44% slower where a few tiles have to fill
+// the chip.  Four stages for T = 128 (a block to a unit): 1 to 10% slower.
 template <typename E, int P, int T>
 __global__ void __launch_bounds__(T == 256 ? 512 : 256)
 ns_product_kernel(NsArgs p) {
@@ -388,7 +397,7 @@ ns_product_kernel(NsArgs p) {
   constexpr bool SYM = P == NS_SYM || P == NS_POLY;
   using TA = RowTile<T, NW>;
   using TB = typename std::conditional<SYM, RowTile<T, NW>, ColTile<T, NW>>::type;
-  constexpr int STAGE = 2 * TA::BYTES + 2 * TB::BYTES;
+  constexpr int STAGE = TA::BYTES + TB::BYTES;
   extern __shared__ __align__(1024) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -403,15 +412,12 @@ ns_product_kernel(NsArgs p) {
   int ti, tj;
   tile_at<P>(p, t, ti, tj);
   const int nk_all = p.K / NS_BK, k0 = nk_all * s / S, nk = nk_all * (s + 1) / S - k0;
-  const int64_t oa = g * p.sa + (int64_t)ti * T * p.lda + k0 * NS_BK;
-  const int64_t ob = g * p.sb + (SYM ? (int64_t)tj * T * p.ldb + k0 * NS_BK : (int64_t)k0 * NS_BK * p.ldb + tj * T);
+  const int64_t oa = g * p.sa + (int64_t)ti * T * p.lda + k0 * 64;
+  const int64_t ob = g * p.sb + (SYM ? (int64_t)tj * T * p.ldb + k0 * 64 : (int64_t)k0 * NS_BK * p.ldb + tj * T * 2);
   auto load = [&](int k) {
     char* st = smem + (k & 1) * STAGE;
-    const int64_t a = oa + k * NS_BK, b = ob + (SYM ? (int64_t)k * NS_BK : (int64_t)k * NS_BK * p.ldb);
-    TA::load(p.Ah + a, p.lda, st, wave, lane);
-    TA::load(p.Al + a, p.lda, st + TA::BYTES, wave, lane);
-    TB::load(p.Bh + b, p.ldb, st + 2 * TA::BYTES, wave, lane);
-    TB::load(p.Bl + b, p.ldb, st + 2 * TA::BYTES + TB::BYTES, wave, lane);
+    TA::load(p.A + oa + k * 64, p.lda, st, wave, lane);
+    TB::load(p.B + ob + (SYM ? (int64_t)k * 64 : (int64_t)k * NS_BK * p.ldb), p.ldb, st + TA::BYTES, wave, lane);
   };
 
   // results along rows (turned: along columns): the lane's 4 consecutive results are the matrix
@@ -432,14 +438,14 @@ ns_product_kernel(NsArgs p) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int c0 = wn * 64 + j * 32;
-      f.bh[j] = TB::frag(st + 2 * TA::BYTES, c0, kk, lane);
-      f.bl[j] = TB::frag(st + 2 * TA::BYTES + TB::BYTES, c0, kk, lane);
+      f.bh[j] = TB::frag(st + TA::BYTES, c0, kk, 0, lane);
+      f.bl[j] = TB::frag(st + TA::BYTES, c0, kk, 1, lane);
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int r0 = wm * (T / WM) + i * 32;
-      f.ah[i] = TA::frag(st, r0, kk, lane);
-      f.al[i] = TA::frag(st + TA::BYTES, r0, kk, lane);
+      f.ah[i] = TA::frag(st, r0, kk, 0, lane);
+      f.al[i] = TA::frag(st, r0, kk, 1, lane);
     }
   };
   auto run = [&](auto TURN) {
@@ -461,7 +467,7 @@ ns_product_kernel(NsArgs p) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mma(f.ah[i], f.bh[j], acc[i][j]);
     };
-    constexpr int LPS = 2 * (TA::PER_WAVE + TB::PER_WAVE);           // loads of a stage, per wave
+    constexpr int LPS = TA::PER_WAVE + TB::PER_WAVE;           // loads of a stage, per wave
     if constexpr (PIPE) {
       // The second half's operands are read before the first half's products, and the next
       // stage's first operands before the second half's, which cover the reads.
@@ -560,11 +566,9 @@ ns_product_kernel(NsArgs p) {
     return;
   }
 
-  // the results split again: 32 rows x 64 columns of each plane at a time through LDS, 128-byte rows
-  f16* Ch = p.Ch + g * p.sc;
-  f16* Cl = p.Cl + g * p.sc;
-  const f16* Xh = p.Ah + g * p.sa;
-  const f16* Xl = p.Al + g * p.sa;
+  // the results split again: 32 rows x 64 columns at a time through LDS, 256-byte rows
+  f16* C = p.C + g * p.sc;
+  const f16* X = p.A + g * p.sa;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int row = i0 + i * 32 + lp;
@@ -575,8 +579,9 @@ ns_product_kernel(NsArgs p) {
         const int col = j0 + j * 32 + 2 * v + lq;
         f16x4_t h4 = {}, l4 = {}, h, l;
         if constexpr (P == NS_POLY) {
-          h4 = *reinterpret_cast<const f16x4_t*>(Xh + (int64_t)row * p.lda + col);
-          l4 = *reinterpret_cast<const f16x4_t*>(Xl + (int64_t)row * p.lda + col);
+          const f16* x = X + at_op(row, col, p.lda);
+          h4 = *reinterpret_cast<const f16x4_t*>(x);
+          l4 = *reinterpret_cast<const f16x4_t*>(x + LO);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -596,9 +601,9 @@ ns_product_kernel(NsArgs p) {
     for (int q = 0; q < 4; ++q) {
       const int r = q * 8 + (lane >> 3), c = lane & 7;
       const char* at = mine + r * 128 + ((c ^ (r & 7)) << 4);
-      const int64_t o = (int64_t)(i0 + i * 32 + r) * p.ldc + j0 + c * 8;
-      *reinterpret_cast<f16x8_t*>(Ch + o) = *reinterpret_cast<const f16x8_t*>(at);
-      *reinterpret_cast<f16x8_t*>(Cl + o) = *reinterpret_cast<const f16x8_t*>(at + 4096);
+      f16* o = C + at_op(i0 + i * 32 + r, j0 + c * 8, p.ldc);
+      *reinterpret_cast<f16x8_t*>(o) = *reinterpret_cast<const f16x8_t*>(at);
+      *reinterpret_cast<f16x8_t*>(o + LO) = *reinterpret_cast<const f16x8_t*>(at + 4096);
     }
     wave_sync();
   }
@@ -625,9 +630,9 @@ ns_product_kernel(NsArgs p) {
       for (int q = 0; q < 8; ++q) {
         const int r = q * 8 + (lane >> 3), c = lane & 7;
         const char* at = mine + r * 128 + ((c ^ (r & 7)) << 4);
-        const int64_t o = (int64_t)(j0 + r) * p.ldc + i0 + i * 32 + c * 8;
-        *reinterpret_cast<f16x8_t*>(Ch + o) = *reinterpret_cast<const f16x8_t*>(at);
-        *reinterpret_cast<f16x8_t*>(Cl + o) = *reinterpret_cast<const f16x8_t*>(at + 8192);
+        f16* o = C + at_op(j0 + r, i0 + i * 32 + c * 8, p.ldc);
+        *reinterpret_cast<f16x8_t*>(o) = *reinterpret_cast<const f16x8_t*>(at);
+        *reinterpret_cast<f16x8_t*>(o + LO) = *reinterpret_cast<const f16x8_t*>(at + 8192);
       }
       wave_sync();
     }
@@ -665,16 +670,16 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
         if (row < p.u.m && col < p.u.n) store_at<E>(p.u, base + col, acc[v][q] * p.down);
       }
   } else {
-    f16* Ch = p.Ch + g * p.sc;
-    f16* Cl = p.Cl + g * p.sc;
+    f16* C = p.C + g * p.sc;
     const int row = i0 + lp;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       const int col = j0 + 8 * v + lq;
       f16x4_t h4 = {}, l4 = {}, h, l;
       if constexpr (P == NS_POLY) {
-        h4 = *reinterpret_cast<const f16x4_t*>(p.Ah + g * p.sa + (int64_t)row * p.lda + col);
-        l4 = *reinterpret_cast<const f16x4_t*>(p.Al + g * p.sa + (int64_t)row * p.lda + col);
+        const f16* x = p.A + g * p.sa + at_op(row, col, p.lda);
+        h4 = *reinterpret_cast<const f16x4_t*>(x);
+        l4 = *reinterpret_cast<const f16x4_t*>(x + LO);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -682,12 +687,14 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
         split(ns_value<P>(acc[v][q], p.down, (float)h4[q], (float)l4[q], row, col + q), vh, vl);
         h[q] = vh; l[q] = vl;
         if ((P == NS_SYM || P == NS_POLY) && ti != tj) {
-          Ch[(int64_t)(col + q) * p.ldc + row] = vh;
-          Cl[(int64_t)(col + q) * p.ldc + row] = vl;
+          f16* o = C + at_op(col + q, row, p.ldc);
+          o[0] = vh;
+          o[LO] = vl;
         }
       }
-      *reinterpret_cast<f16x4_t*>(Ch + (int64_t)row * p.ldc + col) = h;
-      *reinterpret_cast<f16x4_t*>(Cl + (int64_t)row * p.ldc + col) = l;
+      f16* o = C + at_op(row, col, p.ldc);
+      *reinterpret_cast<f16x4_t*>(o) = h;
+      *reinterpret_cast<f16x4_t*>(o + LO) = l;
     }
   }
 }
@@ -949,7 +956,7 @@ struct OrthoPlan {
   int group;                              // matrices at a time
   int slices, nb;                         // fp64 route's slices; blocks of the norm
   int merge;                              // steps to one pass over X
-  size_t part, P, xh[2], xl[2], sh[6], sl[6], sums, total;   // r x r: A, A Q, two of Q, two of their products
+  size_t part, P, x[2], s[6], sums, total;             // s, r x r: A, A Q, two of Q, two of their products
 };
 
 static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
@@ -981,15 +988,14 @@ static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
   o->nb = (int)std::max<int64_t>(1, std::min<int64_t>({NB_MAX, (2048 + o->group - 1) / o->group, q->m * q->n / 4096}));
   const size_t g = (size_t)o->group;
   o->part = off; off += up(g * NB_MAX * sizeof(double));
-  for (size_t* p : {&o->xh[0], &o->xl[0], &o->xh[1], &o->xl[1]}) { *p = off; off += up(g * o->Rp * o->Cp * 2); }
+  for (size_t& p : o->x) { p = off; off += up(g * o->Rp * o->Cp * 4); }
   // Steps to one pass over X (see the top): estimated, the fewest passes against none saved.
   const NsTiling gram = ns_tiling(o->group, true, o->Rp, o->Rp, o->Cp), sym = ns_tiling(o->group, true, o->Rp, o->Rp, o->Rp),
                  pair = ns_tiling(2 * o->group, true, o->Rp, o->Rp, o->Rp), apply = ns_tiling(o->group, false, o->Rp, o->Cp, o->Rp);
   const int most = std::min<int>(q->steps, q->dtype == DMOE_BF16 ? NS_MERGE_BF16 : NS_MERGE_F32);
   const double one = gram.us + sym.us + apply.us, many = gram.us + sym.us + (most - 1) * (2 * sym.us + (most > 2 ? pair.us : 2 * sym.us)) + apply.us;
   o->merge = many < most * one ? most : 1;
-  for (int i = 0; i < (o->merge > 1 ? 6 : 3); ++i)
-    for (size_t* p : {&o->sh[i], &o->sl[i]}) { *p = off; off += up(g * o->Rp * o->Rp * 2); }
+  for (int i = 0; i < (o->merge > 1 ? 6 : 3); ++i) { o->s[i] = off; off += up(g * o->Rp * o->Rp * 4); }
   size_t sums = 0;
   for (int64_t k : {(int64_t)o->group, q->B % o->group})          // whole groups and the last one
     for (const NsTiling& t : {ns_tiling(k, true, o->Rp, o->Rp, o->Cp), ns_tiling(k, true, o->Rp, o->Rp, o->Rp),
@@ -1042,7 +1048,7 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
   auto f = [&](size_t off) { return reinterpret_cast<f16*>(ws + off); };
   double* part = reinterpret_cast<double*>(ws + o.part);
   const int Rp = (int)o.Rp, Cp = (int)o.Cp;
-  const int64_t sx = o.Rp * o.Cp, sr = o.Rp * o.Rp;
+  const int64_t sx = 2 * o.Rp * o.Cp, sr = 2 * o.Rp * o.Rp;
   for (int64_t e0 = 0; e0 < q.B; e0 += o.group) {
     const int g = (int)std::min<int64_t>(o.group, q.B - e0);
     const bool wide = q.m * q.n % Vec<E>::N == 0;
@@ -1050,18 +1056,18 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     DMOE_LAUNCH_NAMED("ortho_norm_kernel", norm, dim3(o.nb, g), dim3(256), 0, st, u, (int)e0, part);
     auto planes = q.n % Vec<E>::N == 0 ? ortho_split_kernel<E, true> : ortho_split_kernel<E, false>;
     DMOE_LAUNCH_NAMED("ortho_split_kernel", planes, dim3(Cp / 64, Rp / 64, g), dim3(256), 0, st, u, (int)e0, part,
-                      o.nb, f(o.xh[0]), f(o.xl[0]), Rp, Cp, sx);
+                      o.nb, f(o.x[0]), Rp, Cp);
     NsArgs p{};
     p.e0 = (int)e0; p.u = u;
     p.part = reinterpret_cast<float*>(ws + o.sums);
     enum { A = 0, AQ = 1, Q0 = 2, P0 = 4 };
-    auto left = [&](int i) { p.Ah = f(o.sh[i]); p.Al = f(o.sl[i]); p.lda = Rp; p.sa = sr; };
-    auto right = [&](int i) { p.Bh = f(o.sh[i]); p.Bl = f(o.sl[i]); p.ldb = Rp; p.sb = sr; };
-    auto to = [&](int i) { p.Ch = f(o.sh[i]); p.Cl = f(o.sl[i]); p.ldc = Rp; p.sc = sr; };
+    auto left = [&](int i) { p.A = f(o.s[i]); p.lda = 2 * Rp; p.sa = sr; };
+    auto right = [&](int i) { p.B = f(o.s[i]); p.ldb = 2 * Rp; p.sb = sr; };
+    auto to = [&](int i) { p.C = f(o.s[i]); p.ldc = 2 * Rp; p.sc = sr; };
     int x = 0;
     for (int k = 0; k < q.steps;) {
       const int merge = std::min(o.merge, q.steps - k);
-      p.Ah = p.Bh = f(o.xh[x]); p.Al = p.Bl = f(o.xl[x]); p.lda = p.ldb = Cp; p.sa = p.sb = sx; p.K = Cp;
+      p.A = p.B = f(o.x[x]); p.lda = p.ldb = 2 * Cp; p.sa = p.sb = sx; p.K = Cp;
       to(A);
       p.down = 1.f / SPLIT;
       ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
@@ -1078,7 +1084,7 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
         if (i + 1 < merge) {               // A of the next step, A Q together with the product
           if (i > 0) {
             p.pair = g;
-            p.Bh2 = f(o.sh[P]); p.Bl2 = f(o.sl[P]); p.Ch2 = f(o.sh[next]); p.Cl2 = f(o.sl[next]);
+            p.B2 = f(o.s[P]); p.C2 = f(o.s[next]);
             p.down2 = 0.25f / SPLIT;
           }
           to(AQ);
@@ -1095,8 +1101,8 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
       }
       k += merge;
       left(P);
-      p.Bh = f(o.xh[x]); p.Bl = f(o.xl[x]); p.ldb = Cp; p.sb = sx;
-      p.Ch = f(o.xh[x ^ 1]); p.Cl = f(o.xl[x ^ 1]); p.ldc = Cp; p.sc = sx;
+      p.B = f(o.x[x]); p.ldb = 2 * Cp; p.sb = sx;
+      p.C = f(o.x[x ^ 1]); p.ldc = 2 * Cp; p.sc = sx;
       p.down = (k < q.steps ? 1.f / SPLIT : 1.f / (SPLIT * SPLIT)) * up;
       if (k < q.steps) ns_product<float, NS_APPLY>(p, g, o.Rp, o.Cp, st);
       else ns_product<E, NS_LAST>(p, g, o.Rp, o.Cp, st);
