@@ -165,10 +165,12 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
   lo = (f16)(v - (float)hi);
 }
 
-// An operand [rows][ld / 2] is held as [rows][ld / 64][hi, lo][32]: a row's 32 values of one LDS stage are
-// 128 contiguous bytes, a whole line of the caches (with a plane each for hi and lo, of which a stage
-// takes half a line at a time: OLDNEW).
-__device__ __forceinline__ int64_t at_op(int64_t row, int col, int64_t ld) { return row * ld + (col >> 5) * 64 + (col & 31); }
+// An operand of `rows` rows is held as [columns / 32][rows][hi, lo][32]: what a tile takes of it for 32 of the
+// contraction is contiguous, or (across it) pieces of 4 KiB, whole cache lines.  Two 4096 x 16384 / 16 of
+// 4096 x 1024 / two 2048 x 8192: 11.6 ms / 2065 us / 2120 us with a plane each for hi and lo, rows of which a
+// stage takes 64 bytes; 11.0 / 1941 / 1957 with 128 bytes of each row (hi and lo side by side) at rows'
+// distance; 11.0 / 1930 / 1920 as it is.
+__device__ __forceinline__ int64_t at_op(int64_t row, int col, int rows) { return ((int64_t)(col >> 5) * rows + row) * 64 + (col & 31); }
 constexpr int LO = 32;                    // from a value's hi to its lo
 
 // X = U / (|U| + eps), an operand [Rp][Cp] padded with zeros; a block to a 64 x 64 piece,
@@ -247,7 +249,7 @@ ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* X, int
       split((float)((double)(turn ? tile[x + k][y] : tile[y][x + k]) * f), vh, vl);
       h[k] = vh; l[k] = vl;
     }
-    f16* o = X + (int64_t)g * 2 * Rp * Cp + at_op(y0 + y, x0 + x, 2 * Cp);
+    f16* o = X + (int64_t)g * 2 * Rp * Cp + at_op(y0 + y, x0 + x, Rp);
     *reinterpret_cast<f16x8_t*>(o) = h;
     *reinterpret_cast<f16x8_t*>(o + LO) = l;
   }
@@ -272,12 +274,10 @@ template <int R, int NW>
 struct RowTile {
   static constexpr int BYTES = R * 128, PER_WAVE = R / 8 / NW;
   static_assert(R % (8 * NW) == 0, "whole instructions to a wave");
-  __device__ __forceinline__ static void load(const f16* base, int ld, char* lds, int wave, int lane) {
-#pragma unroll
-    for (int i = 0; i < PER_WAVE; ++i) {
-      const int q = wave + i * NW, row = q * 8 + lane / 8, c = (lane & 7) ^ ((row >> 1) & 7);
-      g2l(base, ((uint32_t)row * (uint32_t)ld + (uint32_t)(c * 8)) * 2u, lds + q * 1024);
-    }
+  // the wave's i-th load of PER_WAVE
+  __device__ __forceinline__ static void load(const f16* base, char* lds, int i, int wave, int lane) {
+    const int q = wave + i * NW, row = q * 8 + lane / 8, c = (lane & 7) ^ ((row >> 1) & 7);
+    g2l(base, (uint32_t)(row * 128 + c * 16), lds + q * 1024);
   }
   // operand of rows i0 .. i0 + 31 and contraction kk .. kk + 15 (kk = 0 or 16); part: 0 hi, 1 lo
   __device__ __forceinline__ static f16x8_t frag(const char* lds, int i0, int kk, int part, int lane) {
@@ -291,12 +291,9 @@ struct RowTile {
 template <int R, int NW>
 struct ColTile {
   static constexpr int BYTES = R * 128, RPI = 256 / R, PER_WAVE = R / 8 / NW;
-  __device__ __forceinline__ static void load(const f16* base, int ld, char* lds, int wave, int lane) {
-#pragma unroll
-    for (int i = 0; i < PER_WAVE; ++i) {
-      const int q = wave + i * NW, k = q * RPI + lane / (R / 4), c = (lane % (R / 4)) ^ (4 * (k & 3));
-      g2l(base, ((uint32_t)k * (uint32_t)ld + (uint32_t)(c * 8)) * 2u, lds + q * 1024);
-    }
+  __device__ __forceinline__ static void load(const f16* base, int rows, char* lds, int i, int wave, int lane) {
+    const int q = wave + i * NW, k = q * RPI + lane / (R / 4), c = (lane % (R / 4)) ^ (4 * (k & 3));
+    g2l(base, ((uint32_t)(c >> 3) * (uint32_t)rows + (uint32_t)k) * 128u + (uint32_t)(c & 7) * 16u, lds + q * 1024);
   }
   __device__ __forceinline__ static f16x8_t frag(const char* lds, int c0, int kk, int part, int lane) {
     const int g = lane >> 4, i = lane & 15;
@@ -329,7 +326,7 @@ enum NsProduct {
 struct NsArgs {
   const f16 *A, *B;                       // operands, matrix by matrix
   f16* C;                                 // result
-  int lda, ldb, ldc, K;                   // lengths of their rows (twice as many values), multiples of 64; contraction
+  int ra, rb, rc, K;                      // their rows; contraction (multiples of 128)
   int64_t sa, sb, sc;                     // strides of the matrices
   int TI, tiles, total;                   // rows of tiles, tiles of a matrix and of all
   int full, S;                            // tiles past `full` are split into S slices of the contraction:
@@ -381,17 +378,20 @@ __device__ __forceinline__ float ns_value(float acc, float down, float ah, float
 }
 
 // One T x T tile to a block (8 waves of 128 x 64 for T = 256, 4 of 64 x 64 for 128): two LDS stages of
-// 32, the next one loading while the current one is multiplied.  At the 64 bytes a cycle that a CU's LDS
-// was seen to move, a stage's operand reads take 1.3 times the cycles of its products for T = 256 and
-// twice for 128, where two blocks share a unit.  With all units busy the power limit bounds it as much:
-// MFMAs are busy 70% of the time at T = 256, at 1.6 GHz: 1273 TFLOP/s of fp16 products at r = 4096,
-// c = 16384, where a library product of 8192 x 8192 runs at 1470.  Operands straight from memory to
-// registers, kept in their order, no LDS: 5% faster there, 5 to 44% slower where a few tiles have to fill
-// the chip.  Four stages for T = 128 (a block to a unit): 1 to 10% slower.
+// 32, the next one loading while the current one is multiplied.  With all units busy the power limit
+// bounds it: MFMAs are busy 70% of the time at T = 256, at 1.6 to 1.65 GHz: 1310 TFLOP/s of fp16 products
+// at r = 4096, c = 16384, where a library product of 8192 x 8192 runs at 1470.  Operands straight from
+// memory to registers, kept in their order, no LDS: 5% faster there, 5 to 44% slower where a few tiles
+// have to fill the chip.  T = 128: a wave alone on its SIMD stands still while it issues loads and LDS reads
+// one after another, so they lie between its products, the loads first (four 960 x 3008 782 -> 728 us;
+// issued in one go before the products 754).  A stage still takes 0.75 us of a lone block, where its
+// products take 0.35: a third of the loads miss the L2 cache.  Four stages for T = 128: 4 to 9% slower where
+// two blocks would share a unit, -4 to +6% where they do not.
 template <typename E, int P, int T>
 __global__ void __launch_bounds__(T == 256 ? 512 : 256)
 ns_product_kernel(NsArgs p) {
   constexpr int WM = 2, WN = T / 64, NW = WM * WN;
+  constexpr int NST = 2;
   constexpr bool PIPE = T == 128;          // see run(); 256 x 256 tiles have two waves to a SIMD that cover each other
   constexpr int TM = T / WM / 32, TN = 2;
   constexpr bool SYM = P == NS_SYM || P == NS_POLY;
@@ -412,12 +412,18 @@ ns_product_kernel(NsArgs p) {
   int ti, tj;
   tile_at<P>(p, t, ti, tj);
   const int nk_all = p.K / NS_BK, k0 = nk_all * s / S, nk = nk_all * (s + 1) / S - k0;
-  const int64_t oa = g * p.sa + (int64_t)ti * T * p.lda + k0 * 64;
-  const int64_t ob = g * p.sb + (SYM ? (int64_t)tj * T * p.ldb + k0 * 64 : (int64_t)k0 * NS_BK * p.ldb + tj * T * 2);
+  const int64_t oa = g * p.sa + ((int64_t)k0 * p.ra + ti * T) * 64;
+  const int64_t ob = g * p.sb + (SYM ? (int64_t)k0 * p.rb + tj * T : (int64_t)tj * (T / 32) * p.rb + k0 * NS_BK) * 64;
+  constexpr int LPS = TA::PER_WAVE + TB::PER_WAVE;                   // loads of a stage, per wave
+  auto load1 = [&](int k, int i) {
+    char* st = smem + (k % NST) * STAGE;
+    if (i < TA::PER_WAVE) TA::load(p.A + oa + (int64_t)k * p.ra * 64, st, i, wave, lane);
+    else if constexpr (SYM) TB::load(p.B + ob + (int64_t)k * p.rb * 64, st + TA::BYTES, i - TA::PER_WAVE, wave, lane);
+    else TB::load(p.B + ob + (int64_t)k * NS_BK * 64, p.rb, st + TA::BYTES, i - TA::PER_WAVE, wave, lane);
+  };
   auto load = [&](int k) {
-    char* st = smem + (k & 1) * STAGE;
-    TA::load(p.A + oa + k * 64, p.lda, st, wave, lane);
-    TB::load(p.B + ob + (SYM ? (int64_t)k * 64 : (int64_t)k * NS_BK * p.ldb), p.ldb, st + TA::BYTES, wave, lane);
+#pragma unroll
+    for (int i = 0; i < LPS; ++i) load1(k, i);
   };
 
   // results along rows (turned: along columns): the lane's 4 consecutive results are the matrix
@@ -433,74 +439,79 @@ ns_product_kernel(NsArgs p) {
 
   // operands of 16 of the contraction
   struct Frags { f16x8_t ah[TM], al[TM], bh[TN], bl[TN]; };
+  constexpr int NF = 2 * (TM + TN);
+  // the n-th of them, in the order of their use
+  auto read1 = [&](Frags& f, int k, int kk, int n) {
+    const char* st = smem + (k % NST) * STAGE;
+    const int part = n < TM + TN ? n < TN : n >= NF - TM, i = n < TN ? n : n < TM + TN ? n - TN : n < NF - TM ? n - TM - TN : n - NF + TM;
+    if (n < TN || (n >= TM + TN && n < NF - TM)) (part ? f.bl : f.bh)[i] = TB::frag(st + TA::BYTES, wn * 64 + i * 32, kk, part, lane);
+    else (part ? f.al : f.ah)[i] = TA::frag(st, wm * (T / WM) + i * 32, kk, part, lane);
+  };
   auto read = [&](Frags& f, int k, int kk) {
-    const char* st = smem + (k & 1) * STAGE;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int c0 = wn * 64 + j * 32;
-      f.bh[j] = TB::frag(st + TA::BYTES, c0, kk, 0, lane);
-      f.bl[j] = TB::frag(st + TA::BYTES, c0, kk, 1, lane);
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int r0 = wm * (T / WM) + i * 32;
-      f.ah[i] = TA::frag(st, r0, kk, 0, lane);
-      f.al[i] = TA::frag(st, r0, kk, 1, lane);
-    }
+    for (int n = 0; n < NF; ++n) read1(f, k, kk, n);
   };
   auto run = [&](auto TURN) {
     auto mma = [&](const f16x8_t& a, const f16x8_t& b, f32x16_t c) {
       if constexpr (TURN.value) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
       else return __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, c, 0, 0, 0);
     };
-    auto multiply = [&](const Frags& f) {
+    // between the products: between(q) before the q-th of N pieces of other work
+    auto multiply = [&](const Frags& f, auto Nc, auto&& between) {
+      constexpr int MM = 3 * TM * TN, N = decltype(Nc)::value;
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+      for (int q = 0; q < 3; ++q)                                    // hi lo, lo hi, hi hi
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mma(f.ah[i], f.bl[j], acc[i][j]);
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+          for (int j = 0; j < TN; ++j) {
+            acc[i][j] = mma(q == 1 ? f.al[i] : f.ah[i], q == 0 ? f.bl[j] : f.bh[j], acc[i][j]);
+            const int at = (q * TM + i) * TN + j;
+            if (N > 0 && (at + 1) * N / MM > at * N / MM) {
+              __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mma(f.al[i], f.bh[j], acc[i][j]);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mma(f.ah[i], f.bh[j], acc[i][j]);
+              for (int n = at * N / MM; n < (at + 1) * N / MM; ++n) between(n);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
     };
-    constexpr int LPS = TA::PER_WAVE + TB::PER_WAVE;           // loads of a stage, per wave
+    constexpr std::integral_constant<int, 0> none;
+    constexpr std::integral_constant<int, LPS> loads;
     if constexpr (PIPE) {
-      // The second half's operands are read before the first half's products, and the next
-      // stage's first operands before the second half's, which cover the reads.
-      load(0);
-      if (nk > 1) load(1);
-      if (nk > 1) stage_sync<LPS>();
+      // The second half's operands are read between the first half's products, the next stage's first
+      // operands and the loads of the one after it between the second half's.
+#pragma unroll
+      for (int i = 0; i < NST; ++i) if (i < nk) load(i);
+      if (nk >= NST) stage_sync<(NST - 1) * LPS>();
       else stage_sync<0>();
       Frags f0, f1;
       read(f0, 0, 0);
-      for (int k = 0; k < nk; ++k) {
-        read(f1, k, 16);
+      auto step = [&](int k, auto LOADS) {
+        constexpr int n = decltype(LOADS)::value;
+        multiply(f0, std::integral_constant<int, NF>{}, [&](int q) { read1(f1, k, 16, q); });
+        if (n) stage_sync<(NST - 2) * LPS>();
+        else stage_sync<0>();
         __builtin_amdgcn_sched_barrier(0);
-        multiply(f0);
-        __builtin_amdgcn_sched_barrier(0);
-        if (k + 1 < nk) {
-          stage_sync<0>();
-          if (k + 2 < nk) load(k + 2);
-          read(f0, k + 1, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(f1);
-      }
+        multiply(f1, std::integral_constant<int, NF + n>{}, [&](int q) {   // past the last stage: not used
+          if (q < n) load1(k + NST, q);
+          else read1(f0, k + 1, 0, q - n);
+        });
+      };
+      int k = 0;
+      for (; k + NST < nk; ++k) step(k, loads);
+      for (; k < nk; ++k) step(k, none);
     } else {
       load(0);
-      for (int k = 0; k < nk; ++k) {
+      auto step = [&](int k, auto LOADS) {
         stage_sync<0>();
-        if (k + 1 < nk) load(k + 1);
         Frags f;
         read(f, k, 0);
-        multiply(f);
+        multiply(f, LOADS, [&](int q) { load1(k + 1, q); });
         read(f, k, 16);
-        multiply(f);
-      }
+        multiply(f, none, [&](int) {});
+      };
+      for (int k = 0; k + 1 < nk; ++k) step(k, loads);
+      step(nk - 1, none);
     }
   };
   if constexpr (P == NS_LAST) {
@@ -579,7 +590,7 @@ ns_product_kernel(NsArgs p) {
         const int col = j0 + j * 32 + 2 * v + lq;
         f16x4_t h4 = {}, l4 = {}, h, l;
         if constexpr (P == NS_POLY) {
-          const f16* x = X + at_op(row, col, p.lda);
+          const f16* x = X + at_op(row, col, p.ra);
           h4 = *reinterpret_cast<const f16x4_t*>(x);
           l4 = *reinterpret_cast<const f16x4_t*>(x + LO);
         }
@@ -601,7 +612,7 @@ ns_product_kernel(NsArgs p) {
     for (int q = 0; q < 4; ++q) {
       const int r = q * 8 + (lane >> 3), c = lane & 7;
       const char* at = mine + r * 128 + ((c ^ (r & 7)) << 4);
-      f16* o = C + at_op(i0 + i * 32 + r, j0 + c * 8, p.ldc);
+      f16* o = C + at_op(i0 + i * 32 + r, j0 + c * 8, p.rc);
       *reinterpret_cast<f16x8_t*>(o) = *reinterpret_cast<const f16x8_t*>(at);
       *reinterpret_cast<f16x8_t*>(o + LO) = *reinterpret_cast<const f16x8_t*>(at + 4096);
     }
@@ -630,7 +641,7 @@ ns_product_kernel(NsArgs p) {
       for (int q = 0; q < 8; ++q) {
         const int r = q * 8 + (lane >> 3), c = lane & 7;
         const char* at = mine + r * 128 + ((c ^ (r & 7)) << 4);
-        f16* o = C + at_op(j0 + r, i0 + i * 32 + c * 8, p.ldc);
+        f16* o = C + at_op(j0 + r, i0 + i * 32 + c * 8, p.rc);
         *reinterpret_cast<f16x8_t*>(o) = *reinterpret_cast<const f16x8_t*>(at);
         *reinterpret_cast<f16x8_t*>(o + LO) = *reinterpret_cast<const f16x8_t*>(at + 8192);
       }
@@ -677,7 +688,7 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
       const int col = j0 + 8 * v + lq;
       f16x4_t h4 = {}, l4 = {}, h, l;
       if constexpr (P == NS_POLY) {
-        const f16* x = p.A + g * p.sa + at_op(row, col, p.lda);
+        const f16* x = p.A + g * p.sa + at_op(row, col, p.ra);
         h4 = *reinterpret_cast<const f16x4_t*>(x);
         l4 = *reinterpret_cast<const f16x4_t*>(x + LO);
       }
@@ -687,12 +698,12 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
         split(ns_value<P>(acc[v][q], p.down, (float)h4[q], (float)l4[q], row, col + q), vh, vl);
         h[q] = vh; l[q] = vl;
         if ((P == NS_SYM || P == NS_POLY) && ti != tj) {
-          f16* o = C + at_op(col + q, row, p.ldc);
+          f16* o = C + at_op(col + q, row, p.rc);
           o[0] = vh;
           o[LO] = vl;
         }
       }
-      f16* o = C + at_op(row, col, p.ldc);
+      f16* o = C + at_op(row, col, p.rc);
       *reinterpret_cast<f16x4_t*>(o) = h;
       *reinterpret_cast<f16x4_t*>(o + LO) = l;
     }
@@ -927,7 +938,7 @@ gram_apply_kernel(UpdateArgs a, const double* part, int slices, int steps, const
 struct NsTiling { int T, S; int64_t tiles, full, total; double us; };
 
 // 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one.  Measured, us per round of
-// tiles: 2.45 / 1.65 per 32 of the contraction, 0.85 where the smaller ones have a unit to
+// tiles: 2.45 / 1.5 per 32 of the contraction, 0.75 where the smaller ones have a unit to
 // themselves, and the tiles' stores (a symmetric result's twice over).  What a last, partly filled round
 // would take is shortened by slices, at the price of a second launch and the slices' sums
 // through memory (10 to 20 us).
@@ -938,7 +949,7 @@ static NsTiling ns_tiling(int64_t groups, bool sym, int64_t rows, int64_t cols, 
     if (rows % T || cols % T) continue;
     const int64_t a = rows / T, b = cols / T, slots = T == 256 ? 256 : 512;
     const int64_t tiles = sym ? a * (a + 1) / 2 : a * b, total = groups * tiles, rem = total % slots;
-    const double c = T == 256 ? 2.45 : 1.65, alone = T == 256 ? 2.45 : 0.85, store = T == 256 ? (sym ? 20.0 : 8.0) : (sym ? 3.0 : 2.0);
+    const double c = T == 256 ? 2.45 : 1.5, alone = T == 256 ? 2.45 : 0.75, store = T == 256 ? (sym ? 20.0 : 8.0) : (sym ? 3.0 : 2.0);
     for (int S = 1; S <= 32 && (S == 1 || (rem && k >= 8 * S)); ++S) {
       const int64_t blocks = rem * S, last = blocks % slots;
       const double rounds = (double)(blocks / slots) * c + (last == 0 ? 0.0 : last <= 256 ? alone : c);
@@ -1061,13 +1072,13 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     p.e0 = (int)e0; p.u = u;
     p.part = reinterpret_cast<float*>(ws + o.sums);
     enum { A = 0, AQ = 1, Q0 = 2, P0 = 4 };
-    auto left = [&](int i) { p.A = f(o.s[i]); p.lda = 2 * Rp; p.sa = sr; };
-    auto right = [&](int i) { p.B = f(o.s[i]); p.ldb = 2 * Rp; p.sb = sr; };
-    auto to = [&](int i) { p.C = f(o.s[i]); p.ldc = 2 * Rp; p.sc = sr; };
+    auto left = [&](int i) { p.A = f(o.s[i]); p.ra = Rp; p.sa = sr; };
+    auto right = [&](int i) { p.B = f(o.s[i]); p.rb = Rp; p.sb = sr; };
+    auto to = [&](int i) { p.C = f(o.s[i]); p.rc = Rp; p.sc = sr; };
     int x = 0;
     for (int k = 0; k < q.steps;) {
       const int merge = std::min(o.merge, q.steps - k);
-      p.A = p.B = f(o.x[x]); p.lda = p.ldb = 2 * Cp; p.sa = p.sb = sx; p.K = Cp;
+      p.A = p.B = f(o.x[x]); p.ra = p.rb = Rp; p.sa = p.sb = sx; p.K = Cp;
       to(A);
       p.down = 1.f / SPLIT;
       ns_product<float, NS_SYM>(p, g, o.Rp, o.Rp, st);
@@ -1101,8 +1112,8 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
       }
       k += merge;
       left(P);
-      p.B = f(o.x[x]); p.ldb = 2 * Cp; p.sb = sx;
-      p.C = f(o.x[x ^ 1]); p.ldc = 2 * Cp; p.sc = sx;
+      p.B = f(o.x[x]); p.rb = Rp; p.sb = sx;
+      p.C = f(o.x[x ^ 1]); p.rc = Rp; p.sc = sx;
       p.down = (k < q.steps ? 1.f / SPLIT : 1.f / (SPLIT * SPLIT)) * up;
       if (k < q.steps) ns_product<float, NS_APPLY>(p, g, o.Rp, o.Cp, st);
       else ns_product<E, NS_LAST>(p, g, o.Rp, o.Cp, st);
