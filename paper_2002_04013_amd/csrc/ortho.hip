@@ -179,7 +179,10 @@ template <typename E, bool WIDE>
 __global__ void __launch_bounds__(256)
 ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* X, int Rp, int Cp) {
   __shared__ float tile[64][65];
-  __shared__ double inv;
+  // SPLIT / (|U| + eps) = scale 2^up, scale in [0.5, 1]: its range is wider than fp32's.  Bound by memory, at
+  // 5.2 TB/s; with a product in fp64 for each value by the conversions (two 4096 x 16384 154 / 247 us).
+  __shared__ float scale;
+  __shared__ int up;
   const int g = blockIdx.z, e = e0 + g;
   if (!on(a, e)) return;
   if (threadIdx.x < 64) {
@@ -189,7 +192,7 @@ ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* X, int
       if ((int)threadIdx.x + 64 * i < nb) s += part[(int64_t)g * NB_MAX + threadIdx.x + 64 * i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
-    if (threadIdx.x == 0) inv = (double)SPLIT / (sqrt(s) + NS_EPS);
+    if (threadIdx.x == 0) scale = (float)frexp((double)SPLIT / (sqrt(s) + NS_EPS), &up);
   }
   const bool turn = a.m > a.n;
   const int x0 = blockIdx.x * 64, y0 = blockIdx.y * 64;            // column and row of X
@@ -239,14 +242,15 @@ ortho_split_kernel(UpdateArgs a, int e0, const double* part, int nb, f16* X, int
     for (int k = 0; k < 8; ++k) tile[(q + 256 * k) >> 6][q & 63] = u[k];
   }
   __syncthreads();
-  const double f = inv;
+  const float f = scale;
+  const int e2 = up;
   for (int q = threadIdx.x; q < 64 * 8; q += 256) {
     const int y = q >> 3, x = (q & 7) * 8;
     f16x8_t h, l;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       f16 vh, vl;
-      split((float)((double)(turn ? tile[x + k][y] : tile[y][x + k]) * f), vh, vl);
+      split(ldexpf((turn ? tile[x + k][y] : tile[y][x + k]) * f, e2), vh, vl);
       h[k] = vh; l[k] = vl;
     }
     f16* o = X + (int64_t)g * 2 * Rp * Cp + at_op(y0 + y, x0 + x, Rp);
