@@ -7,11 +7,12 @@
 // calls every block of the next launch does it instead); the up-projection, whose blocks each
 // group the pairs by expert for themselves; the down-projection; the weighted average.
 // Measured: 16 tokens of experts 4096 x 16384 (11.1 GB of weights) 1.74 ms, 6.4 TB/s; 37 tokens of experts
-// 1024 x 4096 331 us, 5.2 TB/s; one token of them (67 MB) 28.6 us, of which about 12 are the weights,
+// 1024 x 4096 331 us, 5.2 TB/s; one token of them (67 MB) 27.8 us, of which about 12 are the weights,
 // the rest the chain of the four launches.
 // Slower: the average by the wave that stores the last expert's tile, found by a counter, in place
 // of its launch (the fences cost more: one token 28 -> 31 us, 8 tokens 108 -> 179); a block of the
-// down-projection to 16 columns of all experts (too few blocks: 29 -> 40).
+// down-projection to 16 columns of all experts (too few blocks: 29 -> 40), or to 16 / E columns of all E
+// experts, with the average in it (28.6 -> 28.3, but 4 tokens 67 -> 71, fp32 106 -> 118).
 //
 // The products run on 16-row matrix instructions with the weights as the 16-row operand and
 // an expert's tokens as its 16 columns; no weight is read twice, and the vectors of the
@@ -62,35 +63,45 @@ struct FewArgs {
 
 // ---------------------------------------------------------------- gate
 
-// Scores of four gate columns from c0 for one token by one wave, its lanes at vectors v0 + lane, v0 + lane
-// + step, ...: fp64 multiply-adds of the exact values.  Lane i < 4 returns column c0 + i.
-constexpr int FG_C = 4;
-template <typename E>
+// Scores of C gate columns from c0 for one token by one wave, its lanes at vectors v0 + lane, v0 + lane
+// + step, ...: fp64 multiply-adds of the exact values.  Lane i returns column c0 + i / (64 / C): of a pair of
+// lanes each adds up half of the columns, until one is left (C - 1 + log2(64 / C) exchanges for C log2 64).
+template <typename E, int C>
 __device__ __forceinline__ double few_dot(const GateArgs& a, int t, int c0, int v0, int step) {
   constexpr int VEC = 16 / sizeof(E);
   const int lane = threadIdx.x & 63, nv = a.D / VEC;
   const E* xr = reinterpret_cast<const E*>(a.x) + (int64_t)t * a.D;
   const E* Wg = reinterpret_cast<const E*>(a.Wg);
-  double acc[FG_C] = {0.0, 0.0, 0.0, 0.0};
+  double acc[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) acc[i] = 0.0;
 #pragma unroll 2
   for (int v = v0 + lane; v < nv; v += step) {
     const uint4 fx = *reinterpret_cast<const uint4*>(xr + (int64_t)v * VEC);
-    uint4 fw[FG_C];
+    uint4 fw[C];
 #pragma unroll
-    for (int i = 0; i < FG_C; ++i)
+    for (int i = 0; i < C; ++i)
       fw[i] = *reinterpret_cast<const uint4*>(Wg + (int64_t)min(c0 + i, a.dM - 1) * a.D + (int64_t)v * VEC);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
       const double xj = (double)vec_elem<E>(fx, j);
 #pragma unroll
-      for (int i = 0; i < FG_C; ++i) acc[i] = fma(xj, (double)vec_elem<E>(fw[i], j), acc[i]);
+      for (int i = 0; i < C; ++i) acc[i] = fma(xj, (double)vec_elem<E>(fw[i], j), acc[i]);
     }
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1)
+  for (int n = C / 2; n > 0; n /= 2) {
+    const int o = n * 64 / C;
+    const bool upper = lane & o;
 #pragma unroll
-    for (int i = 0; i < FG_C; ++i) acc[i] += __shfl_xor(acc[i], o, WAVE);
-  return lane == 0 ? acc[0] : lane == 1 ? acc[1] : lane == 2 ? acc[2] : acc[3];
+    for (int i = 0; i < n; ++i) {
+      const double mine = upper ? acc[i + n] : acc[i], other = upper ? acc[i] : acc[i + n];
+      acc[i] = mine + __shfl_xor(other, o, WAVE);
+    }
+  }
+#pragma unroll
+  for (int o = 32 / C; o > 0; o >>= 1) acc[0] += __shfl_xor(acc[0], o, WAVE);
+  return acc[0];
 }
 
 // Choice of experts of token t by one wave from its scores in LDS, exact as dmoe_gate_topk's; lane i < k
@@ -117,7 +128,7 @@ __device__ __forceinline__ int few_choose(const GateArgs& a, const RankTuples& t
 // products over slices of d_model, with the selection in every block of the up-projection (up to 8
 // tokens) or a launch of its own: 37 tokens, 32 columns, D = 1024 16 us for 10; 8 tokens of D = 512 28.7 us
 // a call for 26.6; one token of D = 1024 28.2 for 28.9.
-constexpr int FG_NT = 1024, FG_NW = FG_NT / 64;
+constexpr int FG_NT = 1024, FG_NW = FG_NT / 64, FG_C = 4;
 template <typename E, bool ALIVE>
 __global__ void __launch_bounds__(FG_NT) few_gate_kernel(GateArgs a, int SP, FewPlan* plan) {
   __shared__ double part[FG_NW][DM_MAX];           // SP shares of the columns
@@ -129,8 +140,9 @@ __global__ void __launch_bounds__(FG_NT) few_gate_kernel(GateArgs a, int SP, Few
   const RankTuples tup = rank_tuples<ALIVE>(a);
   for (int u = wv; u < groups * SP; u += FG_NW) {
     const int c0 = u / SP * FG_C, sp = u % SP;
-    const double v = few_dot<E>(a, t, c0, sp * 64, SP * 64);
-    if (lane < FG_C && c0 + lane < a.dM) part[sp][c0 + lane] = v;
+    const double v = few_dot<E, FG_C>(a, t, c0, sp * 64, SP * 64);
+    const int c = c0 + lane / (64 / FG_C);
+    if (lane % (64 / FG_C) == 0 && c < a.dM) part[sp][c] = v;
   }
   __syncthreads();
   if (wv) return;
@@ -151,18 +163,26 @@ struct FewGateLds {
   int chosen[FEW_NW * KMAX];
   float w[FEW_NW * KMAX];
 };
+template <typename E, int C>
+__device__ __forceinline__ void few_scores(const GateArgs& a, FewGateLds& q) {
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (a.dM + C - 1) / C;
+  const E* bg = reinterpret_cast<const E*>(a.bg);
+  for (int u = wv; u < a.T * groups; u += FEW_NW) {
+    const int t = u / groups, c0 = (u - t * groups) * C, c = c0 + lane / (64 / C);
+    const bool mine = lane % (64 / C) == 0 && c < a.dM;
+    const double b = bg && mine ? (double)ldf(bg + c) : 0.0;
+    const double v = few_dot<E, C>(a, t, c0, 0, 64);
+    if (mine) q.s64[t][c] = b + v;
+  }
+}
 template <typename E, bool ALIVE>
 __device__ __forceinline__ void few_gate_block(const GateArgs& a, FewGateLds& q, int* eid) {
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int groups = (a.dM + FG_C - 1) / FG_C;
   const RankTuples tup = rank_tuples<ALIVE>(a);
-  const E* bg = reinterpret_cast<const E*>(a.bg);
-  for (int u = wv; u < a.T * groups; u += FEW_NW) {
-    const int t = u / groups, c = (u - t * groups) * FG_C + lane;
-    const double b = bg && lane < FG_C && c < a.dM ? (double)ldf(bg + c) : 0.0;
-    const double v = few_dot<E>(a, t, c - lane, 0, 64);
-    if (lane < FG_C && c < a.dM) q.s64[t][c] = b + v;
-  }
+  // four columns at a time where that gives every wave work once, else eight
+  if (a.T * a.dM <= 4 * FEW_NW) few_scores<E, 4>(a, q);
+  else few_scores<E, 8>(a, q);
   __syncthreads();
   if (wv < a.T) {
     const int e = few_choose<ALIVE>(a, tup, q.s64[wv], q.scratch[wv], wv, q.chosen, q.w, blockIdx.x == 0);
