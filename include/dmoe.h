@@ -413,7 +413,8 @@ typedef struct {
  * (a, b, c) = (3.4445, -4.7750, 2.0315).  Singular values from about 0.3% of the norm up end in
  * [0.7, 1.21] after five steps; a zero matrix gives zeros.  Products carry about 22 bits or more, whatever the type.
  * counts [B] int32 or NULL: a matrix with counts[e] = 0 (an expert without rows, whose gradient
- * dmoe_expert_ffn_bwd does not write) is not read, and its O left as it is.  O may be G.
+ * dmoe_expert_ffn_bwd does not write) is not read, and its O left as it is.  The other matrices' sums
+ * may be split in other places where some are left out (differences of fp32 rounding).  O may be G.
  * ws: dmoe_orthogonalize_workspace_bytes(mats) bytes (0 for invalid mats), also for
  * dmoe_muon_step. */
 int dmoe_orthogonalize(const dmoe_mats* mats, const void* G, const int32_t* counts, void* O, void* ws,

@@ -163,6 +163,30 @@ def test_left_out_matrices_and_in_place(shape):
     assert torch.equal(_call(c, out=c), ref)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pattern", ["first", "last", "odd", "all", "one"])
+@pytest.mark.parametrize("shape", [(16, 1024, 1024), (300, 70, 200), (30, 520, 300), (130, 512, 1024)], ids=str)
+def test_left_out_matrices_of_many(shape, pattern, dtype):
+    """Batches whose tiles fill the chip, and of several groups, with matrices left out: the others within the bound."""
+    Bn = shape[0]
+    i = torch.arange(Bn, device="cuda")
+    counts = {"first": i >= Bn // 3, "last": i < Bn - 3, "odd": i % 2 == 1, "all": i < 0, "one": i == Bn - 2}[pattern].to(torch.int32) * 5
+    on = counts > 0
+    G = _make(*shape, dtype, 11)
+    keep = G.clone()
+    G[~on] = float("nan")
+    out = _call(G, counts=counts, out=torch.full_like(G, 7.0))
+    assert (out[~on] == 7).all()
+    for j in on.nonzero().flatten().split(40):
+        j = j[::7]
+        ref, err = _steps64(keep[j].double(), 5, bound=True)
+        off = torch.linalg.vector_norm(out[j].double() - ref, dim=(1, 2))
+        assert (off <= err + _half(dtype) * (torch.linalg.vector_norm(ref, dim=(1, 2)) + err)).all(), (off / err).max().item()
+    if pattern == "odd":
+        assert torch.equal(_call(G, counts=counts, out=torch.full_like(G, 7.0)), out)
+
+
 def _muon64(G, mom, W, lr, mu, decay, nesterov):
     mom = mu * mom + G
     o, err = _steps64(G + mu * mom if nesterov else mom, 5, bound=True)
