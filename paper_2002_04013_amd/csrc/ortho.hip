@@ -417,11 +417,13 @@ __device__ __forceinline__ float ns_value(float acc, float down, float ah, float
 // memory to registers, kept in their order, no LDS: 5% faster there, 5 to 44% slower where a few tiles
 // have to fill the chip.  T = 128: a wave alone on its SIMD stands still while it issues loads and LDS reads
 // one after another, so they lie between its products, the loads first (four 960 x 3008 782 -> 728 us;
-// issued in one go before the products 754).  A stage still takes 0.75 us of a lone block, where its
-// products take 0.35: a third of the loads miss the L2 cache.  Four stages for T = 128: 4 to 9% slower where
-// two blocks would share a unit, -4 to +6% where they do not.
-template <typename E, int P, int T>
-__global__ void __launch_bounds__(T == 256 ? 512 : 256)
+// issued in one go before the products 754).  A stage still takes 0.75 us of a block that has its unit to
+// itself, where its products take 0.35: a third of the loads miss the L2 cache.  KG = 2: two groups of
+// four waves with a ring each take half of the contraction each and add up through LDS at the end, 0.55 us
+// a stage (four 960 x 3008 724 -> 672 us, one 1024 x 1024 314 -> 296; of 8 stages and less 3 to 8% slower).  Four
+// stages for T = 128: 4 to 9% slower where two blocks would share a unit, -4 to +6% where they do not.
+template <typename E, int P, int T, int KG>
+__global__ void __launch_bounds__(T == 256 ? 512 : 256 * KG)
 ns_product_kernel(NsArgs p) {
   constexpr int WM = 2, WN = T / 64, NW = WM * WN;
   constexpr int NST = 2;
@@ -432,8 +434,10 @@ ns_product_kernel(NsArgs p) {
   using TB = typename std::conditional<SYM, RowTile<T, NW>, ColTile<T, NW>>::type;
   constexpr int STAGE = TA::BYTES + TB::BYTES;
   extern __shared__ __align__(1024) char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave_b = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = wave_b % NW, kg = wave_b / NW;
   const int wm = wave / WN, wn = wave % WN;
+  char* ring = smem + kg * NST * STAGE;
 
   const bool sliced = (int)blockIdx.x >= p.full;
   const int u = sliced ? xcd_run((int)blockIdx.x - p.full, (int)gridDim.x - p.full) : 0;
@@ -445,12 +449,12 @@ ns_product_kernel(NsArgs p) {
   const int t = L % p.tiles, g = matrix_of<P>(p, L);
   int ti, tj;
   tile_at<P>(p, t, ti, tj);
-  const int nk_all = p.K / NS_BK, k0 = nk_all * s / S, nk = nk_all * (s + 1) / S - k0;
+  const int nk_all = p.K / NS_BK, sk = s * KG + kg, k0 = nk_all * sk / (S * KG), nk = nk_all * (sk + 1) / (S * KG) - k0;
   const int64_t oa = g * p.sa + ((int64_t)k0 * p.ra + ti * T) * 64;
   const int64_t ob = g * p.sb + (SYM ? (int64_t)k0 * p.rb + tj * T : (int64_t)tj * (T / 32) * p.rb + k0 * NS_BK) * 64;
   constexpr int LPS = TA::PER_WAVE + TB::PER_WAVE;                   // loads of a stage, per wave
   auto load1 = [&](int k, int i) {
-    char* st = smem + (k % NST) * STAGE;
+    char* st = ring + (k % NST) * STAGE;
     if (i < TA::PER_WAVE) TA::load(p.A + oa + (int64_t)k * p.ra * 64, st, i, wave, lane);
     else if constexpr (SYM) TB::load(p.B + ob + (int64_t)k * p.rb * 64, st + TA::BYTES, i - TA::PER_WAVE, wave, lane);
     else TB::load(p.B + ob + (int64_t)k * NS_BK * 64, p.rb, st + TA::BYTES, i - TA::PER_WAVE, wave, lane);
@@ -476,7 +480,7 @@ ns_product_kernel(NsArgs p) {
   constexpr int NF = 2 * (TM + TN);
   // the n-th of them, in the order of their use
   auto read1 = [&](Frags& f, int k, int kk, int n) {
-    const char* st = smem + (k % NST) * STAGE;
+    const char* st = ring + (k % NST) * STAGE;
     const int part = n < TM + TN ? n < TN : n >= NF - TM, i = n < TN ? n : n < TM + TN ? n - TN : n < NF - TM ? n - TM - TN : n - NF + TM;
     if (n < TN || (n >= TM + TN && n < NF - TM)) (part ? f.bl : f.bh)[i] = TB::frag(st + TA::BYTES, wn * 64 + i * 32, kk, part, lane);
     else (part ? f.al : f.ah)[i] = TA::frag(st, wm * (T / WM) + i * 32, kk, part, lane);
@@ -555,6 +559,31 @@ ns_product_kernel(NsArgs p) {
     run(std::false_type{});
   }
 
+  stage_sync<0>();                           // the rings are free: 16 KiB of them to a wave
+  if constexpr (KG > 1) {
+    // the second half of the contraction is added to the first
+    f32x4_t* o = reinterpret_cast<f32x4_t*>(smem + NST * STAGE + wave * 16384) + lane;
+    if (kg) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) o[((i * TN + j) * 4 + v) * 64] = f32x4_t{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+    }
+    stage_sync<0>();
+    if (kg) return;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const f32x4_t q = o[((i * TN + j) * 4 + v) * 64];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) acc[i][j][4 * v + x] += q[x];
+        }
+  }
   const int i0 = ti * T + wm * (T / WM), j0 = tj * T + wn * 64;      // the wave's rows and columns
   const int lp = lane & 31, lq = (lane >> 5) * 4;                    // element v: q = 8 (v / 4) + lq + v % 4 of line p = lp
 
@@ -571,7 +600,6 @@ ns_product_kernel(NsArgs p) {
               make_float4(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]);
     return;
   }
-  stage_sync<0>();                           // the ring is free: 16 KiB of it to a wave
   char* mine = smem + wave * 16384;
 
   if constexpr (P == NS_LAST) {
@@ -970,11 +998,12 @@ gram_apply_kernel(UpdateArgs a, const double* part, int slices, int steps, const
 
 // How a product of `groups` matrices is cut: T x T tiles, the tiles past `full` with their contraction
 // in S slices.
-struct NsTiling { int T, S; int64_t tiles, full, total; double us; };
+struct NsTiling { int T, S, KG; int64_t tiles, full, total; double us; };
 
 // 256 x 256 tiles take a compute unit each, 128 x 128 ones half of one.  Measured, us per round of
 // tiles: 2.45 / 1.5 per 32 of the contraction, 0.75 where the smaller ones have a unit to
-// themselves, and the tiles' stores (a symmetric result's twice over).  What a last, partly filled round
+// themselves (with KG = 2, in launches of at most a tile to a unit and 16 stages or more, 0.55 and 1.5 for the
+// sum), and the tiles' stores (a symmetric result's twice over).  What a last, partly filled round
 // would take is shortened by slices, at the price of a second launch and the slices' sums
 // through memory (10 to 20 us).
 static NsTiling ns_tiling(int64_t groups, bool sym, int64_t rows, int64_t cols, int64_t K) {
@@ -984,13 +1013,15 @@ static NsTiling ns_tiling(int64_t groups, bool sym, int64_t rows, int64_t cols, 
     if (rows % T || cols % T) continue;
     const int64_t a = rows / T, b = cols / T, slots = T == 256 ? 256 : 512;
     const int64_t tiles = sym ? a * (a + 1) / 2 : a * b, total = groups * tiles, rem = total % slots;
-    const double c = T == 256 ? 2.45 : 1.5, alone = T == 256 ? 2.45 : 0.75, store = T == 256 ? (sym ? 20.0 : 8.0) : (sym ? 3.0 : 2.0);
+    const double c = T == 256 ? 2.45 : 1.5, store = T == 256 ? (sym ? 20.0 : 8.0) : (sym ? 3.0 : 2.0);
     for (int S = 1; S <= 32 && (S == 1 || (rem && k >= 8 * S)); ++S) {
       const int64_t blocks = rem * S, last = blocks % slots;
+      const int KG = T == 128 && total < slots && blocks <= 256 && k % (2 * S) == 0 && k >= 16 * S ? 2 : 1;
+      const double alone = T == 256 ? 2.45 : KG == 2 ? 0.55 : 0.75;
       const double rounds = (double)(blocks / slots) * c + (last == 0 ? 0.0 : last <= 256 ? alone : c);
       const double us = (double)(total / slots) * ((double)k * c + store) + rounds * (double)((k + S - 1) / S) +
-                        (S > 1 ? 9.0 + (double)(blocks * T * T * 8) / 5e6 : rem ? store : 0.0) + 2.0;
-      if (!best.T || us < best.us) best = NsTiling{T, S, tiles, S > 1 ? total - rem : (total + 7) / 8 * 8, total, us};
+                        (S > 1 ? 9.0 + (double)(blocks * T * T * 8) / 5e6 : rem ? store : 0.0) + 2.0 + (KG == 2 ? 1.5 : 0.0);
+      if (!best.T || us < best.us) best = NsTiling{T, S, KG, tiles, S > 1 ? total - rem : (total + 7) / 8 * 8, total, us};
     }
   }
   return best;
@@ -1061,14 +1092,15 @@ static void ns_product(NsArgs p, int64_t groups, int64_t rows, int64_t cols, hip
     constexpr int T = decltype(Tc)::value;
     p.TI = (int)(rows / T); p.tiles = (int)q.tiles; p.full = (int)q.full; p.S = q.S;
     const int64_t sliced = q.S > 1 ? (q.total - q.full) * q.S : 0;
-    constexpr int lds = 2 * 4 * T * 64;
-    auto kern = ns_product_kernel<E, P, T>;
+    const int64_t blocks = q.full + (sliced + 7) / 8 * 8;
+    const int lds = q.KG * 2 * 4 * T * 64;
+    auto kern = q.KG == 2 ? ns_product_kernel<E, P, T, T == 128 ? 2 : 1> : ns_product_kernel<E, P, T, 1>;
     if (lds > 65536) {
       (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       (void)hipGetLastError();
     }
     const char* name = P == NS_SYM ? "ns_product_kernel (symmetric)" : P == NS_POLY ? "ns_product_kernel (Q)" : "ns_product_kernel (P X)";
-    DMOE_LAUNCH_NAMED(name, kern, dim3((unsigned)(q.full + (sliced + 7) / 8 * 8)), dim3(T == 256 ? 512 : 256), lds, st, p);
+    DMOE_LAUNCH_NAMED(name, kern, dim3((unsigned)blocks), dim3(T == 256 ? 512 : 256 * q.KG), lds, st, p);
     if (sliced)
       DMOE_LAUNCH_NAMED("ns_finish_kernel", (ns_finish_kernel<E, P, T>), dim3((unsigned)((q.total - q.full) * (T / 32) * (T / 32))),
                         dim3(64), 0, st, p);
