@@ -773,6 +773,148 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
   }
 }
 
+// r <= 128: all r x r products of a pass of several steps by one block to a matrix, two operands of 128 x 128 in LDS, in the
+// form of a RowTile's stages; eight waves of 32 x 64, their results in registers until a product's readers
+// are done.  P (the product of the steps, held as above) waits in registers and takes A's place for its own
+// product.  The same sums as the launches one by one, which took 8 us each: bf16 128 x 8152
+// 137 -> 83 us, 50 of 640 x 128 170 -> 91, fp32 33 of 96 x 958 185 -> 146.
+constexpr int ST_N = 128, ST_NT = 512, ST_SLOT = 4 * RowTile<ST_N, 8>::BYTES;
+struct StepsArgs {
+  const f16* A;
+  f16* P;
+  int64_t s;                              // stride of the matrices
+  const int32_t* list;
+  int steps;
+};
+__global__ void __launch_bounds__(ST_NT) ns_steps_kernel(StepsArgs p) {
+  using Tile = RowTile<ST_N, 8>;
+  extern __shared__ __align__(1024) char smem[];
+  if ((int)blockIdx.x >= p.list[0]) return;
+  const int g = p.list[1 + blockIdx.x];
+  char* const X = smem;
+  char* const Y = smem + ST_SLOT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i0 = wave / 2 * 32, j0 = wave % 2 * 64, lp = lane & 31, lq = (lane >> 5) * 4, row = i0 + lp;
+  // four values of a row from column col
+  auto at = [&](char* m, int col, int part) {
+    return reinterpret_cast<f16x4_t*>(m + (col >> 5) * Tile::BYTES + row * 128 + (((4 * part + ((col & 31) >> 3)) ^ ((row >> 1) & 7)) << 4) + (col & 7) * 2);
+  };
+  auto column = [&](int j, int v) { return j0 + j * 32 + 2 * v + lq; };      // of element v (v % 4 == 0) of piece j
+
+  const f16* A = p.A + g * p.s;
+  for (int q = threadIdx.x; q < ST_SLOT / 16; q += ST_NT) {
+    const int b = q >> 10, i = (q >> 3) & 127, c = q & 7;
+    *reinterpret_cast<uint4*>(X + b * Tile::BYTES + i * 128 + ((c ^ ((i >> 1) & 7)) << 4)) = *reinterpret_cast<const uint4*>(A + (int64_t)q * 8);
+  }
+  __syncthreads();
+
+  typedef f32x16_t Piece[2];
+  // a b^T: the transposes of symmetric matrices that differ from symmetric ones by rounding.  With the
+  // products in this order (Q A, then that times Q; Q P) the differences stay small: 3e-4 of the result where the
+  // gradient has rank 10 of 100; with A Q and P Q they grow to 6e-2.
+  auto product = [&](const char* a, const char* b, Piece& acc) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[j][v] = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < ST_N; k += 16) {
+      const char *as = a + (k >> 5) * Tile::BYTES, *bs = b + (k >> 5) * Tile::BYTES;
+      const f16x8_t ah = Tile::frag(as, i0, k & 16, 0, lane), al = Tile::frag(as, i0, k & 16, 1, lane);
+      f16x8_t bh[2], bl[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        bh[j] = Tile::frag(bs, j0 + 32 * j, k & 16, 0, lane);
+        bl[j] = Tile::frag(bs, j0 + 32 * j, k & 16, 1, lane);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bl[j], ah, acc[j], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh[j], al, acc[j], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh[j], ah, acc[j], 0, 0, 0);
+    }
+  };
+  auto scale = [&](Piece& acc, float f) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[j][v] *= f;
+  };
+  // into an operand that no wave reads any more
+  auto store = [&](char* m, const Piece& acc) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4) {
+        f16x4_t h, l;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f16 vh, vl;
+          split(acc[j][v + q], vh, vl);
+          h[q] = vh; l[q] = vl;
+        }
+        *at(m, column(j, v), 0) = h;
+        *at(m, column(j, v), 1) = l;
+      }
+    __syncthreads();
+  };
+
+  Piece acc, P;
+  for (int i = 0; i < p.steps; ++i) {
+    product(X, X, acc);                    // A A
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4) {
+        const f16x4_t h = *at(X, column(j, v), 0), l = *at(X, column(j, v), 1);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc[j][v + q] = ns_value<NS_POLY>(acc[j][v + q], 1.f / SPLIT, (float)h[q], (float)l[q], row, column(j, v) + q);
+      }
+    store(Y, acc);                         // Q
+    const bool more = i + 1 < p.steps;
+    if (i == 0) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) P[j] = acc[j];
+    }
+    if (more) {
+      product(Y, X, acc);                  // Q A
+      scale(acc, 1.f / SPLIT);
+      __syncthreads();
+      store(X, acc);
+      product(X, Y, acc);                  // the next A
+      scale(acc, 1.f / SPLIT);
+    }
+    if (i > 0) {
+      __syncthreads();
+      store(X, P);
+      product(Y, X, P);                    // Q P
+      scale(P, 0.25f / SPLIT);
+    }
+    if (more) {
+      __syncthreads();
+      store(X, acc);
+    }
+  }
+  f16* O = p.P + g * p.s;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4) {
+      f16x4_t h, l;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f16 vh, vl;
+        split(P[j][v + q], vh, vl);
+        h[q] = vh; l[q] = vl;
+      }
+      f16* o = O + at_op(row, column(j, v), ST_N);
+      *reinterpret_cast<f16x4_t*>(o) = h;
+      *reinterpret_cast<f16x4_t*>(o + LO) = l;
+    }
+}
+
 // ---------------------------------------------------------------- r <= 64: the r x r space in fp64
 
 constexpr int GR_COLS = 128;              // columns of X in LDS
@@ -1067,12 +1209,14 @@ static int check_mats(const dmoe_mats* q, OrthoPlan* o) {
   o->part = off; off += up(g * NB_MAX * sizeof(double));
   o->list = off; off += up((g + 1) * sizeof(int32_t));
   for (size_t& p : o->x) { p = off; off += up(g * o->Rp * o->Cp * 4); }
-  // Steps to one pass over X (see the top): estimated, the fewest passes against none saved.
+  // Steps to one pass over X (see the top): estimated, the fewest passes against none saved.  For r <= 128
+  // the fewest are always faster; fp32 keeps to the estimate, which leaves nearly square matrices at
+  // one: there two steps to a pass have several times the error of single ones.
   const NsTiling gram = ns_tiling(o->group, true, o->Rp, o->Rp, o->Cp), sym = ns_tiling(o->group, true, o->Rp, o->Rp, o->Rp),
                  pair = ns_tiling(2 * o->group, true, o->Rp, o->Rp, o->Rp), apply = ns_tiling(o->group, false, o->Rp, o->Cp, o->Rp);
   const int most = std::min<int>(q->steps, q->dtype == DMOE_BF16 ? NS_MERGE_BF16 : NS_MERGE_F32);
   const double one = gram.us + sym.us + apply.us, many = gram.us + sym.us + (most - 1) * (2 * sym.us + (most > 2 ? pair.us : 2 * sym.us)) + apply.us;
-  o->merge = many < most * one ? most : 1;
+  o->merge = (o->Rp == ST_N && q->dtype == DMOE_BF16) || many < most * one ? most : 1;
   for (int i = 0; i < (o->merge > 1 ? 6 : 3); ++i) { o->s[i] = off; off += up(g * o->Rp * o->Rp * 4); }
   size_t sums = 0;
   for (int64_t k : {(int64_t)o->group, q->B % o->group})          // whole groups and the last one
@@ -1154,7 +1298,14 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
       p.K = Rp;
       int P = -1;                          // the steps' product so far, held at SPLIT / 4^(steps - 1)
       float up = 1.f;
-      for (int i = 0; i < merge; ++i) {
+      if (Rp == ST_N && merge > 1) {
+        constexpr int lds = 2 * ST_SLOT;
+        (void)hipFuncSetAttribute((const void*)ns_steps_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        (void)hipGetLastError();
+        DMOE_LAUNCH(ns_steps_kernel, dim3(g), dim3(ST_NT), lds, st, StepsArgs{f(o.s[A]), f(o.s[Q0]), sr, list, merge});
+        P = Q0;
+        for (int i = 1; i < merge; ++i) up *= 4.f;
+      } else for (int i = 0; i < merge; ++i) {
         const int Q = Q0 + (i & 1), next = i == 0 ? Q : P0 + (i & 1);
         left(A); right(A); to(Q);
         p.down = 1.f / SPLIT;

@@ -120,6 +120,18 @@ def test_large_tiles_and_groups(shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2, 128, 128, 5), (3, 70, 700, 9), (2, 900, 128, 20), (300, 100, 150, None), (600, 66, 80, 2), (2, 120, 6000, 1)], ids=str)
+def test_short_side_to_128_of_low_rank(shape):
+    """All steps of a matrix in one block (r <= 128), more matrices than units; steps 2, 5, 6, 7: passes of one and more."""
+    Bn, m, n, rank = shape
+    G = _make(Bn, m, n, "bf16", 3, rank)
+    for steps in (2, 5, 6, 7):
+        ref, err = _steps64(G[::7].double(), steps, bound=True)
+        off = torch.linalg.vector_norm(_call(G, steps)[::7].double() - ref, dim=(1, 2))
+        assert (off <= err + _half("bf16") * (torch.linalg.vector_norm(ref, dim=(1, 2)) + err)).all(), (steps, (off / err).max().item())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
 @pytest.mark.parametrize("shape", [(2, 20, 70), (2, 150, 130)], ids=str)
 def test_other_numbers_of_steps(shape, steps):
