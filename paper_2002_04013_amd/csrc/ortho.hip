@@ -467,13 +467,20 @@ ns_product_kernel(NsArgs p) {
   // results along rows (turned: along columns): the lane's 4 consecutive results are the matrix
   // instruction's first operand's
   const bool turn = P == NS_LAST && p.u.m > p.u.n;
-  f32x16_t acc[TM][TN];
+  // hi lo and lo hi have sums of their own where there are registers to spare, so that the sums of hi hi
+  // are rounded once and not three times for each 16 of the contraction: 2.2e-6 of the result for 2.9e-6 at
+  // 960 x 3008, 0.6% of the time (with two blocks to a unit the registers would cost 15%)
+  constexpr bool LOWS = KG == 2;
+  f32x16_t acc[TM][TN], low[LOWS ? TM : 1][LOWS ? TN : 1];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+      for (int v = 0; v < 16; ++v) {
+        acc[i][j][v] = 0.f;
+        if constexpr (LOWS) low[i][j][v] = 0.f;
+      }
 
   // operands of 16 of the contraction
   struct Frags { f16x8_t ah[TM], al[TM], bh[TN], bl[TN]; };
@@ -503,7 +510,8 @@ ns_product_kernel(NsArgs p) {
         for (int i = 0; i < TM; ++i)
 #pragma unroll
           for (int j = 0; j < TN; ++j) {
-            acc[i][j] = mma(q == 1 ? f.al[i] : f.ah[i], q == 0 ? f.bl[j] : f.bh[j], acc[i][j]);
+            f32x16_t& c = LOWS && q < 2 ? low[LOWS ? i : 0][LOWS ? j : 0] : acc[i][j];
+            c = mma(q == 1 ? f.al[i] : f.ah[i], q == 0 ? f.bl[j] : f.bh[j], c);
             const int at = (q * TM + i) * TN + j;
             if (N > 0 && (at + 1) * N / MM > at * N / MM) {
               __builtin_amdgcn_sched_barrier(0);
@@ -559,6 +567,11 @@ ns_product_kernel(NsArgs p) {
     run(std::false_type{});
   }
 
+  if constexpr (LOWS)
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] += low[i][j];
   stage_sync<0>();                           // the rings are free: 16 KiB of them to a wave
   if constexpr (KG > 1) {
     // the second half of the contraction is added to the first
@@ -786,6 +799,7 @@ struct StepsArgs {
   const int32_t* list;
   int steps;
 };
+template <bool LOWS>
 __global__ void __launch_bounds__(ST_NT) ns_steps_kernel(StepsArgs p) {
   using Tile = RowTile<ST_N, 8>;
   extern __shared__ __align__(1024) char smem[];
@@ -813,10 +827,12 @@ __global__ void __launch_bounds__(ST_NT) ns_steps_kernel(StepsArgs p) {
   // products in this order (Q A, then that times Q; Q P) the differences stay small: 3e-4 of the result where the
   // gradient has rank 10 of 100; with A Q and P Q they grow to 6e-2.
   auto product = [&](const char* a, const char* b, Piece& acc) {
+    Piece sums;                            // of hi lo and lo hi (LOWS), as in ns_product_kernel
+    Piece& low = LOWS ? sums : acc;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[j][v] = 0.f;
+      for (int v = 0; v < 16; ++v) acc[j][v] = low[j][v] = 0.f;
 #pragma unroll 2
     for (int k = 0; k < ST_N; k += 16) {
       const char *as = a + (k >> 5) * Tile::BYTES, *bs = b + (k >> 5) * Tile::BYTES;
@@ -828,12 +844,15 @@ __global__ void __launch_bounds__(ST_NT) ns_steps_kernel(StepsArgs p) {
         bl[j] = Tile::frag(bs, j0 + 32 * j, k & 16, 1, lane);
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bl[j], ah, acc[j], 0, 0, 0);
+      for (int j = 0; j < 2; ++j) low[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bl[j], ah, low[j], 0, 0, 0);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh[j], al, acc[j], 0, 0, 0);
+      for (int j = 0; j < 2; ++j) low[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh[j], al, low[j], 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh[j], ah, acc[j], 0, 0, 0);
     }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if constexpr (LOWS) acc[j] += low[j];
   };
   auto scale = [&](Piece& acc, float f) {
 #pragma unroll
@@ -1300,9 +1319,11 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
       float up = 1.f;
       if (Rp == ST_N && merge > 1) {
         constexpr int lds = 2 * ST_SLOT;
-        (void)hipFuncSetAttribute((const void*)ns_steps_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        // an fp32 result gets the sums of the low parts apart (3 to 4% of a call)
+        auto kern = sizeof(E) == 4 ? ns_steps_kernel<true> : ns_steps_kernel<false>;
+        (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         (void)hipGetLastError();
-        DMOE_LAUNCH(ns_steps_kernel, dim3(g), dim3(ST_NT), lds, st, StepsArgs{f(o.s[A]), f(o.s[Q0]), sr, list, merge});
+        DMOE_LAUNCH_NAMED("ns_steps_kernel", kern, dim3(g), dim3(ST_NT), lds, st, StepsArgs{f(o.s[A]), f(o.s[Q0]), sr, list, merge});
         P = Q0;
         for (int i = 1; i < merge; ++i) up *= 4.f;
       } else for (int i = 0; i < merge; ++i) {
