@@ -11,18 +11,19 @@
 // r > 64: the products on fp16 matrix instructions with every operand as the sum of two fp16
 // values, x 2^14 = hi + lo (22 bits; every entry is at most 3.45 in magnitude: the singular
 // values stay below 1.21, A's below 1.45, and a I + b A + c A A lies between 0.6 and a), and
-// three products hi hi + hi lo + lo hi into one fp32 accumulator.  A and Q = a I + b A + c A A are
+// three products hi hi + hi lo + lo hi into fp32 accumulators.  A and Q = a I + b A + c A A are
 // symmetric: tiles of the lower triangle only, stored twice.  Bound by the fp16 matrix rate:
 // 3 (r^2 c + r^3 + 2 r^2 c) flops for a single step.
 //
 // Several steps share a pass over X: with P = Q_k .. Q_1 and A_(k+1) = Q_k A_k Q_k, all polynomials of
 // the first A and so symmetric, X <- P X.  Every further step costs four symmetric products of r^3 in
 // place of one, X X^T and Q X.  The price is that A_k is no longer formed from a rounded X: what
-// rounding leaves in A grows by a^2 a step.  Two steps to a pass have the error of single steps or
-// less (1.8e-6 to 5e-5 of the result, as plain fp32; simulated spectra: full rank, ranks 8 to 256 with
-// and without noise, one to eight dominant directions, powers), five 2e-6 to 4e-4: fp32 takes two and
-// bf16, which rounds the result by 1.7e-3, five, where that is the shorter by the estimates of
-// ns_tiling.
+// rounding leaves in A grows by a^2 a step.  fp32 takes the first two steps together, where A's largest
+// values are not yet near one, and single steps after them, which take back most of it: errors of 0.8e-6 to
+// 2.1e-6 of the result, a plain fp32 evaluation's 1.0e-6 to 3.4e-6; the next two together as well: up to 2.6e-6 where
+// that has 1.7e-6 (200 x 6000).  bf16, which rounds the result by 1.7e-3, takes five to a pass (2e-6 to 4e-4
+// over simulated spectra: full rank, ranks 8 to 256 with and without noise, one to eight dominant directions,
+// powers).  Both where it is the shorter by the estimates of ns_tiling.
 //
 // r <= 64: everything in the r x r space in fp64.  X_k = P_k X_0 with P_k a polynomial of
 // A_0 = X_0 X_0^T, so  Q = a I + b A + c A A,  P <- Q P,  A <- Q A Q  from A_0, P_0 = I, and
@@ -416,11 +417,11 @@ __device__ __forceinline__ float ns_value(float acc, float down, float ah, float
 // at r = 4096, c = 16384, where a library product of 8192 x 8192 runs at 1470.  Operands straight from
 // memory to registers, kept in their order, no LDS: 5% faster there, 5 to 44% slower where a few tiles
 // have to fill the chip.  T = 128: a wave alone on its SIMD stands still while it issues loads and LDS reads
-// one after another, so they lie between its products, the loads first (four 960 x 3008 782 -> 728 us;
-// issued in one go before the products 754).  A stage still takes 0.75 us of a block that has its unit to
+// one after another, so they lie between its products, the loads first (144 tiles of K = 1024 34 -> 29 us;
+// the loads alone between them 30 to 32).  A stage still takes 0.75 us of a block that has its unit to
 // itself, where its products take 0.35: a third of the loads miss the L2 cache.  KG = 2: two groups of
 // four waves with a ring each take half of the contraction each and add up through LDS at the end, 0.55 us
-// a stage (four 960 x 3008 724 -> 672 us, one 1024 x 1024 314 -> 296; of 8 stages and less 3 to 8% slower).  Four
+// a stage (144 tiles of K = 1024 29 -> 25 us, one bf16 1024 x 1024 a call 314 -> 296; of 8 stages and less 3 to 8% slower).  Four
 // stages for T = 128: 4 to 9% slower where two blocks would share a unit, -4 to +6% where they do not.
 template <typename E, int P, int T, int KG>
 __global__ void __launch_bounds__(T == 256 ? 512 : 256 * KG)
@@ -468,7 +469,7 @@ ns_product_kernel(NsArgs p) {
   // instruction's first operand's
   const bool turn = P == NS_LAST && p.u.m > p.u.n;
   // hi lo and lo hi have sums of their own where there are registers to spare, so that the sums of hi hi
-  // are rounded once and not three times for each 16 of the contraction: 2.2e-6 of the result for 2.9e-6 at
+  // are rounded once and not three times for each 16 of the contraction: a quarter less of an error at
   // 960 x 3008, 0.6% of the time (with two blocks to a unit the registers would cost 15%)
   constexpr bool LOWS = KG == 2;
   f32x16_t acc[TM][TN], low[LOWS ? TM : 1][LOWS ? TN : 1];
@@ -790,7 +791,7 @@ __global__ void __launch_bounds__(64) ns_finish_kernel(NsArgs p) {
 // form of a RowTile's stages; eight waves of 32 x 64, their results in registers until a product's readers
 // are done.  P (the product of the steps, held as above) waits in registers and takes A's place for its own
 // product.  The same sums as the launches one by one, which took 8 us each: bf16 128 x 8152
-// 137 -> 83 us, 50 of 640 x 128 170 -> 91, fp32 33 of 96 x 958 185 -> 146.
+// 137 -> 83 us, 50 of 640 x 128 170 -> 91.
 constexpr int ST_N = 128, ST_NT = 512, ST_SLOT = 4 * RowTile<ST_N, 8>::BYTES;
 struct StepsArgs {
   const f16* A;
@@ -1309,7 +1310,8 @@ static void orthogonalize(const dmoe_mats& q, const OrthoPlan& o, UpdateArgs u, 
     auto to = [&](int i) { p.C = f(o.s[i]); p.rc = Rp; p.sc = sr; };
     int x = 0;
     for (int k = 0; k < q.steps;) {
-      const int merge = std::min(o.merge, q.steps - k);
+      // fp32: the first pass only (see the top)
+      const int merge = std::min(k == 0 || sizeof(E) == 2 ? o.merge : 1, q.steps - k);
       p.A = p.B = f(o.x[x]); p.ra = p.rb = Rp; p.sa = p.sb = sx; p.K = Cp;
       to(A);
       p.down = 1.f / SPLIT;
